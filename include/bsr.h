@@ -377,6 +377,81 @@ int32_t bsr_attention_backward(const void* qkv_dev, const void* dout_dev, const 
                                int32_t dtype, int32_t batch, int32_t t, int32_t heads, int32_t d, void* dqkv_dev_out,
                                float* delta_scratch_dev, int32_t use_tensor_cores, void* stream);
 
+/* ---- rows of an expert layer and products in 8-bit blocks ------------------------------------
+ *
+ * What an expert layer outside the step is built from (Section 5.2 gives the layer; the step's own layers keep their kernels):
+ * slots sorted by expert, the tokens' rows in that order, the experts' products over them, and the weighted sum
+ * per token, each with its gradient:
+ *
+ *   forward   bsr_expert_sort; bsr_expert_scatter_e4m3; bsr_expert_linear_e4m3_block128 (GELU, pre-activation kept);
+ *             bsr_quantize_e4m3_rows128; bsr_expert_linear_e4m3_block128; bsr_expert_combine
+ *   backward  bsr_expert_combine_backward; bsr_quantize_e4m3_rows128; bsr_expert_linear_e4m3_block128 with the second layer's
+ *             transposed copy (times GELU'); the same with the first layer's; bsr_expert_combine without weights
+ *
+ * The experts' weights are frozen here (Eq. 2: their input gradient needs the weights alone).  A user's program quantises them once.
+ *
+ * E4M3 in blocks of 128: values in groups of 128 along a row (activations) or 128 x 128 (weights) share a power of two
+ * 2^e, e the least integer with max|x| <= 448 * 2^e (0 for a block of zeros), and are held as round_e4m3(x * 2^-e), to nearest and even.
+ * The scale is the byte e + 127; a row of scales over k values is bsr_e4m3_scale_stride(k) bytes, four for every 512 values, of which
+ * those behind the last block hold 127.  A value that is not finite has no part in its block's scale and becomes
+ * NaN, so that the other rows and columns of a product stay what they are.
+ * Pointers to rows, weights, codes, biases and outputs are 16-byte aligned, those to scales 4-byte aligned. */
+
+/* Bytes of a row of scales over k values: 4 * ceil(k / 512).  Host-only; 0 if k < 1. */
+int32_t bsr_e4m3_scale_stride(int32_t k);
+
+/* Positions of the slots in the order of (expert, token, slot).  expert_dev [tokens, top_k] int32: the expert of every slot; any
+ * value outside [0, experts) means that the slot has none (a padded token).
+ *   pos_dev_out        [tokens, top_k] int32: the slot's row, -1 without an expert
+ *   seg_start_dev_out  [experts + 1] int32: expert e has the rows seg_start[e] .. seg_start[e + 1] - 1
+ * tokens >= 0, top_k >= 1, tokens * top_k <= 2^30, 1 <= experts <= 1024.  A token may have the same expert twice. */
+int32_t bsr_expert_sort(const int32_t* expert_dev, int32_t tokens, int32_t top_k, int32_t experts, int32_t* pos_dev_out,
+                        int32_t* seg_start_dev_out, void* stream);
+
+/* rows[pos[t, s]] = x[t] for every slot that has a row.  x [tokens, dim] and rows_dev_out [tokens * top_k, dim] in `dtype`;
+ * pos as bsr_expert_sort writes it (a position outside the rows counts as none); rows behind the last one stay as they
+ * were.  dim * sizeof(dtype) must be a multiple of 16.  The gradient of x is bsr_expert_combine without weights and residual. */
+int32_t bsr_expert_scatter(const void* x_dev, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos_dev,
+                           void* rows_dev_out, void* stream);
+/* The same with the rows in E4M3 blocks: codes_dev_out [tokens * top_k, dim] and scale_dev_out [tokens * top_k,
+ * bsr_e4m3_scale_stride(dim)], as bsr_quantize_e4m3_rows128 would make them from the scattered rows.  dim a multiple of 16. */
+int32_t bsr_expert_scatter_e4m3(const void* x_dev, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos_dev,
+                                void* codes_dev_out, void* scale_dev_out, void* stream);
+
+/* out[t] = residual[t] + sum over the slots s of t that have a row of weights[t, s] * rows[pos[t, s]], summed in float32 in slot order.
+ * rows [tokens * top_k, dim] in `rows_dtype`; weights [tokens, top_k] float32 or NULL (ones); residual (or NULL) and
+ * out_dev_out [tokens, dim] in `dtype` (they may be the same buffer).  What a slot without a row has for a weight is not read. */
+int32_t bsr_expert_combine(const void* rows_dev, int32_t rows_dtype, const int32_t* pos_dev, const float* weights_dev, const void* residual_dev,
+                           void* out_dev_out, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, void* stream);
+/* Its gradients: drows[pos[t, s]] = weights[t, s] * dout[t] (in `rows_dtype`; rows behind the last one stay as they were) and
+ * dweights[t, s] = <dout[t], rows[pos[t, s]]> float32, 0 for a slot without a row.  The residual's gradient is dout itself. */
+int32_t bsr_expert_combine_backward(const void* dout_dev, int32_t dtype, const void* rows_dev, int32_t rows_dtype, const int32_t* pos_dev,
+                                    const float* weights_dev, void* drows_dev_out, float* dweights_dev_out, int32_t tokens, int32_t dim,
+                                    int32_t top_k, void* stream);
+
+/* Rows x [m, k] in `dtype` to codes [m, k] and scales [m, bsr_e4m3_scale_stride(k)]; k a multiple of 16. */
+int32_t bsr_quantize_e4m3_rows128(const void* x_dev, int32_t dtype, int32_t m, int32_t k, void* codes_dev_out, void* scale_dev_out, void* stream);
+/* Stacked weights w [count, n, k] in `dtype` to codes [count, n, k] and scales [count, ceil(n / 128), bsr_e4m3_scale_stride(k)].  With
+ * codes_t_dev_out (then scale_t_dev_out too; else both NULL) also the transposed copies [count, k, n] with scales [count,
+ * ceil(k / 128), bsr_e4m3_scale_stride(n)], which a product reads as weights to form an input gradient.  k a multiple of 16,
+ * n too for transposed copies; count <= 65535, n <= 128 * 65535. */
+int32_t bsr_quantize_e4m3_blocks128(const void* w_dev, int32_t dtype, int32_t count, int32_t n, int32_t k, void* codes_dev_out, void* scale_dev_out,
+                                    void* codes_t_dev_out, void* scale_t_dev_out, void* stream);
+
+/* y = act(x W^T + bias) of such operands, accumulated in float32.  x [m, k], w [n, k], bias [n] float32 or NULL, y [m, n]
+ * bf16; k a multiple of 16, n of 8.  act: BSR_ACT_NONE (z NULL); BSR_ACT_GELU, with the pre-activation written to z [m, n] bf16 unless
+ * it is NULL; BSR_ACT_GELU_GRAD: x W^T + bias times GELU'(z), z read. */
+enum { BSR_ACT_NONE = 0, BSR_ACT_GELU = 1, BSR_ACT_GELU_GRAD = 2 };
+int32_t bsr_linear_forward_e4m3_block128(const void* x_codes_dev, const void* x_scale_dev, const void* w_codes_dev, const void* w_scale_dev,
+                                         const float* bias_dev, void* z_dev, void* y_dev, int32_t m, int32_t n, int32_t k, int32_t act,
+                                         void* stream);
+/* The same over rows sorted by expert: the rows seg_start[e] .. seg_start[e + 1] - 1 of x [m, k] with w [experts, n, k][e] and bias
+ * [experts, n][e].  Rows of y and z outside every segment stay as they were.  1 <= experts <= 1024, experts * n < 2^31; seg_start
+ * as bsr_expert_sort writes it (what lies outside [0, m] is cut, and a row that two segments name is the later one's). */
+int32_t bsr_expert_linear_e4m3_block128(const void* x_codes_dev, const void* x_scale_dev, const void* w_codes_dev, const void* w_scale_dev,
+                                        const float* bias_dev, const int32_t* seg_start_dev, void* z_dev, void* y_dev, int32_t m, int32_t n,
+                                        int32_t k, int32_t experts, int32_t act, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

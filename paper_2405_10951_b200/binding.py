@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libbsr_checked.so" if os.environ.get("BSR_LIBRAR
 
 BSR_OK = 0
 DTYPE_FP32, DTYPE_BF16 = 0, 1
+ACT_NONE, ACT_GELU, ACT_GELU_GRAD = 0, 1, 2
 MAX_DROPS, MAX_TASKS, MAX_DEPTH = 8, 4, 32
 
 STATUS_NAMES = {0: "BSR_OK", -1: "BSR_ERR_INVALID_ARG", -2: "BSR_ERR_UNSUPPORTED", -3: "BSR_ERR_WORKSPACE_TOO_SMALL",
@@ -27,7 +28,9 @@ STATUS_NAMES = {0: "BSR_OK", -1: "BSR_ERR_INVALID_ARG", -2: "BSR_ERR_UNSUPPORTED
 EXPORTS = ["bsr_token_schedule", "bsr_workspace_bytes", "bsr_create", "bsr_destroy", "bsr_last_error", "bsr_set_param",
            "bsr_get_tensor", "bsr_set_lr", "bsr_set_step", "bsr_train_step", "bsr_train_steps", "bsr_train_step_host", "bsr_forward_backward", "bsr_grad_buffer", "bsr_optimizer_step", "bsr_eval_forward", "bsr_get_footprint",
            "bsr_sync_status", "bsr_selftest_wait_expiry", "bsr_set_gemm_mode", "bsr_set_graph_mode", "bsr_profile_enable", "bsr_profile_read", "bsr_profile_launches", "bsr_token_select", "bsr_gather_fuse", "bsr_linear_forward", "bsr_linear_forward_e4m3", "bsr_linear_backward",
-           "bsr_linear_backward_static", "bsr_static_last_error", "bsr_attention_forward", "bsr_attention_backward"]
+           "bsr_linear_backward_static", "bsr_static_last_error", "bsr_attention_forward", "bsr_attention_backward",
+           "bsr_e4m3_scale_stride", "bsr_expert_sort", "bsr_expert_scatter", "bsr_expert_scatter_e4m3", "bsr_expert_combine", "bsr_expert_combine_backward",
+           "bsr_quantize_e4m3_rows128", "bsr_quantize_e4m3_blocks128", "bsr_linear_forward_e4m3_block128", "bsr_expert_linear_e4m3_block128"]
 
 
 class bsr_dims(C.Structure):
@@ -115,6 +118,16 @@ def lib() -> C.CDLL:
         L.bsr_static_last_error.argtypes = []
         L.bsr_attention_forward.argtypes = [vp, i32, i32, i32, i32, i32, vp, f32p, f32p, i32, vp]
         L.bsr_attention_backward.argtypes = [vp, vp, f32p, f32p, i32, i32, i32, i32, i32, vp, f32p, i32, vp]
+        L.bsr_e4m3_scale_stride.argtypes = [i32]
+        L.bsr_expert_sort.argtypes = [i32p, i32, i32, i32, i32p, i32p, vp]
+        L.bsr_expert_scatter.argtypes = [vp, i32, i32, i32, i32, i32p, vp, vp]
+        L.bsr_expert_scatter_e4m3.argtypes = [vp, i32, i32, i32, i32, i32p, vp, vp, vp]
+        L.bsr_expert_combine.argtypes = [vp, i32, i32p, f32p, vp, vp, i32, i32, i32, i32, vp]
+        L.bsr_expert_combine_backward.argtypes = [vp, i32, vp, i32, i32p, f32p, vp, f32p, i32, i32, i32, vp]
+        L.bsr_quantize_e4m3_rows128.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+        L.bsr_quantize_e4m3_blocks128.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.bsr_linear_forward_e4m3_block128.argtypes = [vp, vp, vp, vp, f32p, vp, vp, i32, i32, i32, i32, vp]
+        L.bsr_expert_linear_e4m3_block128.argtypes = [vp, vp, vp, vp, f32p, i32p, vp, vp, i32, i32, i32, i32, i32, vp]
         for name in EXPORTS:
             if name not in ("bsr_last_error", "bsr_static_last_error"):
                 getattr(L, name).restype = C.c_int32
@@ -280,6 +293,227 @@ def bsr_attention_backward(qkv, dout, lse, score_grad=None, use_tensor_cores: bo
     _check(lib().bsr_attention_backward(_ptr(qkv), _ptr(dout), _ptr(lse), _ptr(score_grad), dt, B, T, H, d, _ptr(dqkv), _ptr(delta),
                                         int(use_tensor_cores), _stream()))
     return dqkv
+
+
+# ---- rows of an expert layer, products in 8-bit blocks of 128 -----------------------------------
+# Outputs may be passed in (a decoding loop or a captured graph keeps its buffers); what is not is allocated.  The library sees
+# pointers alone, so types, shapes, contiguity and devices are checked here.
+def _same_device(*tensors):
+    import torch
+    device = torch.device("cuda", torch.cuda.current_device())
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise BsrError(-1, f"tensor on {t.device}: the call runs on the current device, {device}")
+
+
+def _takes(name, t, dtypes, shape):
+    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise BsrError(-1, f"{name} must be a contiguous tensor of {' or '.join(map(str, dtypes))} and shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _float_type(name, t):
+    import torch
+    if t.dtype is torch.float32:
+        return DTYPE_FP32
+    if t.dtype is torch.bfloat16:
+        return DTYPE_BF16
+    raise BsrError(-1, f"{name} must be float32 or bfloat16, not {t.dtype}")
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def bsr_e4m3_scale_stride(k: int) -> int:
+    """Bytes of a row of scales over k values."""
+    return (k + 511) // 512 * 4 if k >= 1 else 0
+
+
+def bsr_expert_sort(expert, experts: int, pos=None, seg_start=None):
+    """expert: int32 [tokens, top_k], values outside [0, experts) for slots without an expert.  Returns (pos [tokens, top_k], seg_start
+    [experts + 1]) int32."""
+    import torch
+    tokens, top_k = expert.shape
+    _takes("expert", expert, (torch.int32,), (tokens, top_k))
+    if pos is None:
+        pos = torch.empty_like(expert)
+    if seg_start is None:
+        seg_start = torch.empty(max(experts, 0) + 1, dtype=torch.int32, device=expert.device)
+    _takes("pos", pos, (torch.int32,), (tokens, top_k))
+    _takes("seg_start", seg_start, (torch.int32,), (experts + 1,))
+    _same_device(expert, pos, seg_start)
+    _check(lib().bsr_expert_sort(_at(expert), tokens, top_k, experts, _at(pos), _at(seg_start), _stream()))
+    return pos, seg_start
+
+
+def bsr_expert_scatter(x, pos, rows=None):
+    """x [tokens, dim] to rows [tokens * top_k, dim] in the order of pos."""
+    import torch
+    tokens, dim = x.shape
+    top_k = pos.shape[1]
+    dt = _float_type("x", x)
+    if rows is None:
+        rows = torch.empty((tokens * top_k, dim), dtype=x.dtype, device=x.device)
+    _takes("x", x, (x.dtype,), (tokens, dim))
+    _takes("pos", pos, (torch.int32,), (tokens, top_k))
+    _takes("rows", rows, (x.dtype,), (tokens * top_k, dim))
+    _same_device(x, pos, rows)
+    _check(lib().bsr_expert_scatter(_at(x), dt, tokens, dim, top_k, _at(pos), _at(rows), _stream()))
+    return rows
+
+
+def bsr_expert_scatter_e4m3(x, pos, q=None, scale=None):
+    """The same in E4M3 blocks of 128: returns (codes [tokens * top_k, dim] float8_e4m3fn, scales [tokens * top_k, stride] uint8)."""
+    import torch
+    tokens, dim = x.shape
+    top_k = pos.shape[1]
+    dt = _float_type("x", x)
+    q, scale = _codes_out(x, (tokens * top_k, dim), q, scale)
+    _takes("x", x, (x.dtype,), (tokens, dim))
+    _takes("pos", pos, (torch.int32,), (tokens, top_k))
+    _same_device(x, pos, q, scale)
+    _check(lib().bsr_expert_scatter_e4m3(_at(x), dt, tokens, dim, top_k, _at(pos), _at(q), _at(scale), _stream()))
+    return q, scale
+
+
+def bsr_expert_combine(rows, pos, weights=None, residual=None, out=None, dtype=None):
+    """residual + the weighted sum of every token's rows, in the type of out (or of residual, `dtype`, rows).  Without weights and residual: the
+    gradient of bsr_expert_scatter."""
+    import torch
+    tokens, top_k = pos.shape
+    dim = rows.shape[1]
+    if out is None:
+        out = torch.empty((tokens, dim), dtype=residual.dtype if residual is not None else dtype or rows.dtype, device=rows.device)
+    rt, ot = _float_type("rows", rows), _float_type("out", out)
+    _takes("rows", rows, (rows.dtype,), (tokens * top_k, dim))
+    _takes("pos", pos, (torch.int32,), (tokens, top_k))
+    _takes("out", out, (out.dtype,), (tokens, dim))
+    if weights is not None:
+        _takes("weights", weights, (torch.float32,), (tokens, top_k))
+    if residual is not None:
+        _takes("residual", residual, (out.dtype,), (tokens, dim))
+    _same_device(rows, pos, weights, residual, out)
+    _check(lib().bsr_expert_combine(_at(rows), rt, _at(pos), _at(weights), _at(residual), _at(out), ot, tokens, dim, top_k, _stream()))
+    return out
+
+
+def bsr_expert_combine_backward(dout, rows, pos, weights, drows=None, dw=None):
+    """Returns (drows [tokens * top_k, dim] in the type of rows, dw [tokens, top_k] float32)."""
+    import torch
+    tokens, top_k = pos.shape
+    dim = rows.shape[1]
+    if drows is None:
+        drows = torch.empty_like(rows)
+    if dw is None:
+        dw = torch.empty((tokens, top_k), dtype=torch.float32, device=rows.device)
+    ot, rt = _float_type("dout", dout), _float_type("rows", rows)
+    _takes("dout", dout, (dout.dtype,), (tokens, dim))
+    _takes("rows", rows, (rows.dtype,), (tokens * top_k, dim))
+    _takes("pos", pos, (torch.int32,), (tokens, top_k))
+    _takes("weights", weights, (torch.float32,), (tokens, top_k))
+    _takes("drows", drows, (rows.dtype,), (tokens * top_k, dim))
+    _takes("dw", dw, (torch.float32,), (tokens, top_k))
+    _same_device(dout, rows, pos, weights, drows, dw)
+    _check(lib().bsr_expert_combine_backward(_at(dout), ot, _at(rows), rt, _at(pos), _at(weights), _at(drows), _at(dw), tokens, dim, top_k, _stream()))
+    return drows, dw
+
+
+def _code_types():
+    import torch
+    return (torch.float8_e4m3fn, torch.uint8)
+
+
+def _codes_out(like, shape, q, scale, name=""):
+    """Codes of `shape` and a row of scales a row (scale_rows: shape[:-1])."""
+    import torch
+    if q is None:
+        q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=like.device)
+    at = tuple(shape[:-1]) + (bsr_e4m3_scale_stride(shape[-1]),)
+    if scale is None:
+        scale = torch.empty(at, dtype=torch.uint8, device=like.device)
+    _takes("codes" + name, q, _code_types(), shape)
+    _takes("scale" + name, scale, (torch.uint8,), at)
+    return q, scale
+
+
+def bsr_quantize_e4m3_rows128(x, q=None, scale=None):
+    """x [m, k] to (codes [m, k] float8_e4m3fn, scales [m, stride] uint8)."""
+    m, k = x.shape
+    dt = _float_type("x", x)
+    q, scale = _codes_out(x, (m, k), q, scale)
+    _takes("x", x, (x.dtype,), (m, k))
+    _same_device(x, q, scale)
+    _check(lib().bsr_quantize_e4m3_rows128(_at(x), dt, m, k, _at(q), _at(scale), _stream()))
+    return q, scale
+
+
+def bsr_quantize_e4m3_blocks128(w, transposed: bool = False, q=None, scale=None, qt=None, scale_t=None):
+    """w [n, k] or [count, n, k] to (codes, scales [..., ceil(n / 128), stride]); with `transposed` (or qt and scale_t) also the transposed
+    copies [..., k, n] and their scales."""
+    import torch
+    if w.dim() not in (2, 3):
+        raise BsrError(-1, "w must be [n, k] or [count, n, k]")
+    n, k = w.shape[-2:]
+    stack = tuple(w.shape[:-2])
+    dt = _float_type("w", w)
+    _takes("w", w, (w.dtype,), stack + (n, k))
+
+    def outputs(q, scale, n, k, name=""):
+        at = stack + ((n + 127) // 128, bsr_e4m3_scale_stride(k))
+        if q is None:
+            q = torch.empty(stack + (n, k), dtype=torch.float8_e4m3fn, device=w.device)
+        if scale is None:
+            scale = torch.empty(at, dtype=torch.uint8, device=w.device)
+        _takes("codes" + name, q, _code_types(), stack + (n, k))
+        _takes("scale" + name, scale, (torch.uint8,), at)
+        return q, scale
+
+    q, scale = outputs(q, scale, n, k)
+    if transposed or qt is not None or scale_t is not None:
+        qt, scale_t = outputs(qt, scale_t, k, n, "_t")
+    _same_device(w, q, scale, qt, scale_t)
+    _check(lib().bsr_quantize_e4m3_blocks128(_at(w), dt, stack[0] if stack else 1, n, k, _at(q), _at(scale), _at(qt), _at(scale_t), _stream()))
+    return (q, scale) if qt is None else (q, scale, qt, scale_t)
+
+
+def _block128_operands(xq, xs, wq, ws, stack, bias, act, z, y):
+    import torch
+    m, k = xq.shape
+    n = wq.shape[-2]
+    if y is None:
+        y = torch.empty((m, n), dtype=torch.bfloat16, device=xq.device)
+    codes, bf = _code_types(), (torch.bfloat16,)
+    _takes("xq", xq, codes, (m, k))
+    _takes("xs", xs, (torch.uint8,), (m, bsr_e4m3_scale_stride(k)))
+    _takes("wq", wq, codes, stack + (n, k))
+    _takes("ws", ws, (torch.uint8,), stack + ((n + 127) // 128, bsr_e4m3_scale_stride(k)))
+    _takes("y", y, bf, (m, n))
+    if bias is not None:
+        _takes("bias", bias, (torch.float32,), stack + (n,))
+    if z is not None:
+        _takes("z", z, bf, (m, n))
+    return m, n, k, y
+
+
+def bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, bias=None, act: int = ACT_NONE, z=None, y=None):
+    """y [m, n] bf16 = act(x W^T + bias) from the codes and scales of x [m, k] and W [n, k].  act ACT_GELU: the pre-activation goes to z
+    [m, n] bf16 if that is given; ACT_GELU_GRAD: the product is multiplied by GELU'(z)."""
+    m, n, k, y = _block128_operands(xq, xs, wq, ws, (), bias, act, z, y)
+    _same_device(xq, xs, wq, ws, bias, z, y)
+    _check(lib().bsr_linear_forward_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(z), _at(y), m, n, k, act, _stream()))
+    return y
+
+
+def bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg_start, bias=None, act: int = ACT_NONE, z=None, y=None):
+    """The same with a weight per expert: rows seg_start[e] .. seg_start[e + 1] - 1 of x with W[e], wq [experts, n, k], bias [experts, n].  Rows of y and
+    z outside every segment stay as they are (a y that is not passed in holds anything there)."""
+    import torch
+    experts = wq.shape[0]
+    m, n, k, y = _block128_operands(xq, xs, wq, ws, (experts,), bias, act, z, y)
+    _takes("seg_start", seg_start, (torch.int32,), (experts + 1,))
+    _same_device(xq, xs, wq, ws, seg_start, bias, z, y)
+    _check(lib().bsr_expert_linear_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(seg_start), _at(z), _at(y), m, n, k, experts, act, _stream()))
+    return y
 
 
 class Engine:

@@ -1,0 +1,170 @@
+// Quantisation to E4M3 with a power-of-two scale per block of 128 values (a row's) or 128 x 128 values (a weight's):
+//
+//   e = the least integer with max|x| <= 448 * 2^e over the block's finite values,   q = E4M3(x * 2^-e), to nearest and even
+//
+// A scale is held as the byte e + 127.  Being a power of two it costs no rounding: x * 2^-e is exact, so that every code is the one nearest
+// to x / scale, and the tensor core's block scaling multiplies by it exactly.  (A scale of max / 448 itself would use up to one more
+// bit of the largest exponent, which a floating-point code does not need.)  Values that are not finite become the NaN code and have no
+// part in the scale: only their own rows and columns of a product are lost.  Bytes per value are what bounds both kernels.
+#include "block128.cuh"
+#include "common.cuh"
+#include "kernels.h"
+
+namespace bsr {
+
+// Rows of x to codes and scales, a warp per 512 values of a row: a lane has 16 of them, eight lanes a block, and the four blocks'
+// bytes make one word of scales.  With `pos`, token t's codes go to the rows pos[t, 0 .. top_k) (negative: none) of what is
+// written, which has `rows` of them; without it to row t.
+template <typename T, bool SCATTER>
+__global__ void __launch_bounds__(256)
+quantize_rows128_kernel(const T* __restrict__ x, int m, int k, int groups, const int* __restrict__ pos, int top_k, unsigned rows,
+                        uint8_t* __restrict__ q, uint32_t* __restrict__ scale) {
+  dependent_sync();
+  const long unit = ((long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31;
+  if (unit >= (long)m * groups) return;
+  const int row = (int)(unit / groups), g = (int)(unit - (long)row * groups), col = g * 512 + lane * 16;
+  Codes16 c;
+  float v[16];
+  if (col < k) load_values16(x + (size_t)row * k + col, v);
+  else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = 0.f;
+  }
+  uint32_t top = finite_max16(v);
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const uint32_t byte = scale_byte(top);
+  c = codes16(v, byte);
+  const uint32_t word = __shfl_sync(0xffffffffu, byte, 0) | __shfl_sync(0xffffffffu, byte, 8) << 8 | __shfl_sync(0xffffffffu, byte, 16) << 16 |
+                        __shfl_sync(0xffffffffu, byte, 24) << 24;
+  if constexpr (SCATTER) {
+    for (int s = 0; s < top_k; ++s) {
+      const unsigned to = (unsigned)pos[(size_t)row * top_k + s];
+      if (to >= rows) continue;
+      if (col < k) *reinterpret_cast<uint4*>(q + (size_t)to * k + col) = c.u;
+      if (lane == 0) scale[(size_t)to * groups + g] = word;
+    }
+  } else {
+    if (col < k) *reinterpret_cast<uint4*>(q + (size_t)row * k + col) = c.u;
+    if (lane == 0) scale[(size_t)row * groups + g] = word;
+  }
+}
+
+// Stacked matrices w [count, n, k]: a CTA per block of 128 x 128, which it holds in registers (16 columns of four rows a thread).  With
+// qt also the transposed copies [count, k, n] and their scales: a block's scale is the same either way, and its codes are turned in
+// shared memory, four by four.
+constexpr int QB_THREADS = 256;
+template <typename T>
+__global__ void __launch_bounds__(QB_THREADS)
+quantize_blocks128_kernel(const T* __restrict__ w, int n, int k, uint8_t* __restrict__ q, uint8_t* __restrict__ scale, int stride,
+                          uint8_t* __restrict__ qt, uint8_t* __restrict__ scale_t, int stride_t) {
+  dependent_sync();
+  __shared__ uint32_t tops[QB_THREADS / 32];
+  __shared__ uint32_t tile[128 * 33];
+  const int kb = blockIdx.x, nb = blockIdx.y;
+  const size_t mat = blockIdx.z;
+  const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 16, col = kb * 128 + c0;
+  w += mat * n * k;
+  q += mat * n * k;
+  float v[4][16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = nb * 128 + r0 + 32 * i;
+    if (row < n && col < k) load_values16(w + (size_t)row * k + col, v[i]);
+    else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[i][j] = 0.f;
+    }
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max(top, finite_max16(v[i]));
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < QB_THREADS / 32; ++i) top = max(top, tops[i]);
+  const uint32_t byte = scale_byte(top);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + 32 * i, row = nb * 128 + r;
+    const Codes16 c = codes16(v[i], byte);
+    if (row < n && col < k) *reinterpret_cast<uint4*>(q + (size_t)row * k + col) = c.u;
+    if (qt != nullptr) {
+      const uint32_t* u = reinterpret_cast<const uint32_t*>(&c.u);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) tile[r * 33 + c0 / 4 + j] = u[j];
+    }
+  }
+  // scales: the thread of the block's first column writes its byte, the last block's threads the padding behind it
+  const int kblocks = (k + 127) / 128, nblocks = (n + 127) / 128;
+  if (threadIdx.x == 0) scale[(mat * nblocks + nb) * stride + kb] = (uint8_t)byte;
+  if (kb == kblocks - 1 && threadIdx.x < stride - kblocks) scale[(mat * nblocks + nb) * stride + kblocks + threadIdx.x] = 127;
+  if (qt == nullptr) return;
+  if (threadIdx.x == 0) scale_t[(mat * kblocks + kb) * stride_t + nb] = (uint8_t)byte;
+  if (nb == nblocks - 1 && threadIdx.x < stride_t - nblocks) scale_t[(mat * kblocks + kb) * stride_t + nblocks + threadIdx.x] = 127;
+  __syncthreads();
+  // a thread turns four 4 x 4 squares of a word column (four values of k): rows n 16 a .. 16 a + 15, and writes 16 bytes a value of k
+  const int kw = threadIdx.x & 31, a = threadIdx.x >> 5;
+  uint32_t out[4][4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    uint32_t x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = tile[(a * 16 + s * 4 + j) * 33 + kw];
+    const uint32_t p0 = __byte_perm(x[0], x[1], 0x5140), p1 = __byte_perm(x[2], x[3], 0x5140);
+    const uint32_t p2 = __byte_perm(x[0], x[1], 0x7362), p3 = __byte_perm(x[2], x[3], 0x7362);
+    out[0][s] = __byte_perm(p0, p1, 0x5410);
+    out[1][s] = __byte_perm(p0, p1, 0x7632);
+    out[2][s] = __byte_perm(p2, p3, 0x5410);
+    out[3][s] = __byte_perm(p2, p3, 0x7632);
+  }
+  __syncthreads();
+  // through shared memory once more, so that a row of the transposed copy leaves 128 bytes at a time
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) tile[(kw * 4 + j) * 33 + a * 4 + s] = out[j][s];
+  __syncthreads();
+  qt += mat * n * k;
+  const int ncol = nb * 128 + c0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + 32 * i, krow = kb * 128 + r;
+    if (krow < k && ncol < n) {
+      uint4 u;
+      u.x = tile[r * 33 + c0 / 4]; u.y = tile[r * 33 + c0 / 4 + 1]; u.z = tile[r * 33 + c0 / 4 + 2]; u.w = tile[r * 33 + c0 / 4 + 3];
+      *reinterpret_cast<uint4*>(qt + (size_t)krow * n + ncol) = u;
+    }
+  }
+}
+
+int scale_stride128(int k) { return (k + 511) / 512 * 4; }
+
+template <typename T>
+static void quantize_rows(const Ctx& c, const void* x, int m, int k, const int* pos, int top_k, void* q, void* scale) {
+  const int groups = scale_stride128(k) / 4;
+  const long blocks = ((long)m * groups + 7) / 8;
+  note_launch(1);
+  if (pos != nullptr)
+    launch_k(quantize_rows128_kernel<T, true>, (unsigned)blocks, 256, 0, c.stream, (const T*)x, m, k, groups, pos, top_k, (unsigned)m * (unsigned)top_k, (uint8_t*)q, (uint32_t*)scale);
+  else
+    launch_k(quantize_rows128_kernel<T, false>, (unsigned)blocks, 256, 0, c.stream, (const T*)x, m, k, groups, pos, top_k, 0u, (uint8_t*)q, (uint32_t*)scale);
+}
+
+void quantize_rows128(const Ctx& c, const void* x, int m, int k, const int* pos, int top_k, void* q, void* scale) {
+  if (c.dtype == 0) quantize_rows<float>(c, x, m, k, pos, top_k, q, scale);
+  else quantize_rows<bf16>(c, x, m, k, pos, top_k, q, scale);
+}
+
+void quantize_blocks128(const Ctx& c, const void* w, int count, int n, int k, void* q, void* scale, void* qt, void* scale_t) {
+  const dim3 grid(ceil_div(k, 128), ceil_div(n, 128), count);
+  note_launch(1);
+  if (c.dtype == 0)
+    launch_k(quantize_blocks128_kernel<float>, grid, QB_THREADS, 0, c.stream, (const float*)w, n, k, (uint8_t*)q, (uint8_t*)scale, scale_stride128(k), (uint8_t*)qt, (uint8_t*)scale_t, scale_stride128(n));
+  else
+    launch_k(quantize_blocks128_kernel<bf16>, grid, QB_THREADS, 0, c.stream, (const bf16*)w, n, k, (uint8_t*)q, (uint8_t*)scale, scale_stride128(k), (uint8_t*)qt, (uint8_t*)scale_t, scale_stride128(n));
+}
+
+}  // namespace bsr

@@ -8,6 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <string>
 #include <vector>
@@ -1783,6 +1784,130 @@ int32_t bsr_attention_backward(const void* qkv, const void* dout, const float* l
   if (attention_bwd(c, qkv, nullptr, dout, lse, delta_scratch, score_grad, dqkv, batch, t, heads, d) != 0)
     return set_err(g_error, BSR_ERR_UNSUPPORTED, "%d tokens do not fit the attention kernel's shared memory", t);
   return check_cuda(nullptr, "bsr_attention_backward");
+}
+
+// ---- rows of an expert layer, products in 8-bit blocks -------------------------------------------
+
+static bool unaligned(std::initializer_list<const void*> ps, uintptr_t to = 16) {
+  for (const void* p : ps)
+    if (((uintptr_t)p & (to - 1)) != 0) return true;
+  return false;
+}
+static bool bad_dtype(int32_t d) { return d != BSR_DTYPE_FP32 && d != BSR_DTYPE_BF16; }
+// Sizes that the calls on (token, slot) pairs share; rows of `dtype` are whole 16-byte units.
+static int check_slots(int32_t tokens, int32_t dim, int32_t top_k, int32_t dtype) {
+  if (tokens < 0 || top_k < 1 || (int64_t)tokens * top_k > (1 << 30)) return set_err(g_error, BSR_ERR_INVALID_ARG, "need tokens >= 0, top_k >= 1 and tokens * top_k <= 2^30");
+  if (dim < 1 || (dim * dtype_size(dtype)) % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad shape: rows must be a multiple of 16 bytes");
+  return BSR_OK;
+}
+
+int32_t bsr_e4m3_scale_stride(int32_t k) { return k < 1 ? 0 : scale_stride128(k); }
+
+int32_t bsr_expert_sort(const int32_t* expert, int32_t tokens, int32_t top_k, int32_t experts, int32_t* pos, int32_t* seg_start, void* stream) {
+  if (tokens < 0 || top_k < 1 || (int64_t)tokens * top_k > (1 << 30)) return set_err(g_error, BSR_ERR_INVALID_ARG, "need tokens >= 0, top_k >= 1 and tokens * top_k <= 2^30");
+  if (experts < 1 || experts > 1024) return set_err(g_error, BSR_ERR_INVALID_ARG, "experts must be in [1, 1024]");
+  if (seg_start == nullptr || (tokens > 0 && (expert == nullptr || pos == nullptr))) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (expert_sort(bare_ctx(BSR_DTYPE_FP32, stream), expert, tokens * top_k, experts, pos, seg_start) != 0)
+    return set_err(g_error, BSR_ERR_CUDA, "bsr_expert_sort: shared memory could not be reserved");
+  return check_cuda(nullptr, "bsr_expert_sort");
+}
+
+int32_t bsr_expert_scatter(const void* x, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos, void* rows, void* stream) {
+  if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
+  if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
+  if (tokens == 0) return BSR_OK;
+  if (x == nullptr || pos == nullptr || rows == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (unaligned({x, rows})) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned");
+  expert_scatter(bare_ctx(dtype, stream), x, tokens, dim, top_k, pos, rows);
+  return check_cuda(nullptr, "bsr_expert_scatter");
+}
+
+int32_t bsr_expert_scatter_e4m3(const void* x, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos, void* codes,
+                                void* scale, void* stream) {
+  if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
+  if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
+  if (dim % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "dim must be a multiple of 16");
+  if (tokens == 0) return BSR_OK;
+  if (x == nullptr || pos == nullptr || codes == nullptr || scale == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (unaligned({x, codes}) || unaligned({scale}, 4)) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned, scales 4-byte");
+  quantize_rows128(bare_ctx(dtype, stream), x, tokens, dim, pos, top_k, codes, scale);
+  return check_cuda(nullptr, "bsr_expert_scatter_e4m3");
+}
+
+int32_t bsr_expert_combine(const void* rows, int32_t rows_dtype, const int32_t* pos, const float* weights, const void* residual, void* out, int32_t dtype,
+                           int32_t tokens, int32_t dim, int32_t top_k, void* stream) {
+  if (bad_dtype(dtype) || bad_dtype(rows_dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
+  if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
+  if (int rc = check_slots(tokens, dim, top_k, rows_dtype)) return rc;
+  if (tokens == 0) return BSR_OK;
+  if (rows == nullptr || pos == nullptr || out == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (unaligned({rows, residual, out})) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned");
+  expert_combine(bare_ctx(dtype, stream), rows, rows_dtype, pos, weights, residual, out, tokens, dim, top_k);
+  return check_cuda(nullptr, "bsr_expert_combine");
+}
+
+int32_t bsr_expert_combine_backward(const void* dout, int32_t dtype, const void* rows, int32_t rows_dtype, const int32_t* pos, const float* weights, void* drows,
+                                    float* dweights, int32_t tokens, int32_t dim, int32_t top_k, void* stream) {
+  if (bad_dtype(dtype) || bad_dtype(rows_dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
+  if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
+  if (int rc = check_slots(tokens, dim, top_k, rows_dtype)) return rc;
+  if (tokens == 0) return BSR_OK;
+  if (dout == nullptr || rows == nullptr || pos == nullptr || weights == nullptr || drows == nullptr || dweights == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (unaligned({dout, rows, drows})) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned");
+  expert_combine_bwd(bare_ctx(dtype, stream), dout, rows, rows_dtype, pos, weights, drows, dweights, tokens, dim, top_k);
+  return check_cuda(nullptr, "bsr_expert_combine_backward");
+}
+
+int32_t bsr_quantize_e4m3_rows128(const void* x, int32_t dtype, int32_t m, int32_t k, void* codes, void* scale, void* stream) {
+  if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
+  if (m < 0 || k < 16 || k % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0 and k a multiple of 16");
+  if (m == 0) return BSR_OK;
+  if (x == nullptr || codes == nullptr || scale == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (unaligned({x, codes}) || unaligned({scale}, 4)) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned, scales 4-byte");
+  quantize_rows128(bare_ctx(dtype, stream), x, m, k, nullptr, 1, codes, scale);
+  return check_cuda(nullptr, "bsr_quantize_e4m3_rows128");
+}
+
+int32_t bsr_quantize_e4m3_blocks128(const void* w, int32_t dtype, int32_t count, int32_t n, int32_t k, void* codes, void* scale, void* codes_t, void* scale_t,
+                                    void* stream) {
+  if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
+  if (count < 1 || count > 65535 || n < 1 || n > 128 * 65535 || k < 16 || k % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "need 1 <= count <= 65535, 1 <= n <= 128 * 65535 and k a multiple of 16");
+  if (w == nullptr || codes == nullptr || scale == nullptr || (codes_t == nullptr) != (scale_t == nullptr)) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (codes_t != nullptr && n % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "transposed copies need n a multiple of 16");
+  if (unaligned({w, codes, codes_t}) || unaligned({scale, scale_t}, 4)) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned, scales 4-byte");
+  quantize_blocks128(bare_ctx(dtype, stream), w, count, n, k, codes, scale, codes_t, scale_t);
+  return check_cuda(nullptr, "bsr_quantize_e4m3_blocks128");
+}
+
+static int32_t linear_block128(const char* what, const void* x, const void* xs, const void* w, const void* ws, const float* bias, const int32_t* seg_start, void* z, void* y,
+                               int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, void* stream) {
+  if (m < 0 || n < 8 || n % 8 != 0 || k < 16 || k % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0, n a multiple of 8 and k a multiple of 16");
+  if (act < BSR_ACT_NONE || act > BSR_ACT_GELU_GRAD) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad act");
+  if (m == 0) return BSR_OK;
+  if (x == nullptr || xs == nullptr || w == nullptr || ws == nullptr || y == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (act == BSR_ACT_NONE && z != nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "a pre-activation belongs to an activation");
+  if (act == BSR_ACT_GELU_GRAD && z == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "GELU' needs the pre-activation z");
+  if (unaligned({x, w, bias, z, y}) || unaligned({xs, ws}, 4)) return set_err(g_error, BSR_ERR_INVALID_ARG, "operands must be 16-byte aligned, scales 4-byte");
+  GemmEpilogue e;
+  e.bias = bias;
+  e.act = act;
+  if (act == BSR_ACT_GELU) e.aux_out = z;
+  if (act == BSR_ACT_GELU_GRAD) e.aux_in = z;
+  if (gemm_block128(bare_ctx(BSR_DTYPE_BF16, stream), x, xs, w, ws, seg_start, experts, y, m, n, k, e) != 0)
+    return set_err(g_error, BSR_ERR_CUDA, "%s: set-up failed", what);
+  return check_cuda(nullptr, what);
+}
+
+int32_t bsr_linear_forward_e4m3_block128(const void* x, const void* xs, const void* w, const void* ws, const float* bias, void* z, void* y, int32_t m, int32_t n,
+                                         int32_t k, int32_t act, void* stream) {
+  return linear_block128("bsr_linear_forward_e4m3_block128", x, xs, w, ws, bias, nullptr, z, y, m, n, k, 1, act, stream);
+}
+
+int32_t bsr_expert_linear_e4m3_block128(const void* x, const void* xs, const void* w, const void* ws, const float* bias, const int32_t* seg_start, void* z, void* y,
+                                        int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, void* stream) {
+  if (experts < 1 || experts > 1024 || (int64_t)experts * n > INT32_MAX) return set_err(g_error, BSR_ERR_INVALID_ARG, "need 1 <= experts <= 1024 and experts * n < 2^31");
+  if (seg_start == nullptr && m > 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  return linear_block128("bsr_expert_linear_e4m3_block128", x, xs, w, ws, bias, seg_start, z, y, m, n, k, experts, act, stream);
 }
 
 }  // extern "C"

@@ -312,6 +312,21 @@ void moe_gate_bwd(const Ctx& c, const MoeBufs& b, const void* dxg, const float* 
 void moe_gate_wgrad(const Ctx& c, const MoeBufs& b, const float* dsel_row, const int* task_ids, int tokens_per_image, int tasks, int D,
                     int E, float* dwg);
 
+// ---- rows of an expert layer outside the step (expert_rows.cu) and E4M3 in blocks of 128 (block128.cu, gemm_block128.cu) -------------
+// pos [slots]: place of every slot in the order of its expert, -1 without one; seg_start [E + 1].  E <= 1024.
+int expert_sort(const Ctx& c, const int* expert, int slots, int E, int* pos, int* seg_start);
+void expert_scatter(const Ctx& c, const void* x, int tokens, int dim, int top_k, const int* pos, void* rows);
+// c.dtype is that of out, residual and dout; w and residual are optional.
+void expert_combine(const Ctx& c, const void* rows, int rows_dtype, const int* pos, const float* w, const void* residual, void* out, int tokens, int dim, int top_k);
+void expert_combine_bwd(const Ctx& c, const void* dout, const void* rows, int rows_dtype, const int* pos, const float* w, void* drows, float* dw, int tokens, int dim, int top_k);
+int scale_stride128(int k);
+// Rows (c.dtype) to codes and scales; with pos, token t's to the rows pos[t, 0 .. top_k).
+void quantize_rows128(const Ctx& c, const void* x, int m, int k, const int* pos, int top_k, void* q, void* scale);
+void quantize_blocks128(const Ctx& c, const void* w, int count, int n, int k, void* q, void* scale, void* qt, void* scale_t);
+// C [m, n] bf16 from codes and scales; seg_start null: dense, experts 1.  e: bias ([experts][n]), act, aux_out, aux_in.
+int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void* Wq, const void* w_scale, const int* seg_start, int experts, void* C, int m, int n, int k,
+                  const GemmEpilogue& e);
+
 // ---- guard words between workspace slices ------------------------------------------------------
 // table[i]: byte offset from base of guard i (words 32-bit values each).  guards_write fills them with `word`;
 // guards_check raises STATUS_GUARD in *status when any word differs.

@@ -414,7 +414,8 @@ int32_t bsr_expert_sort(const int32_t* expert_dev, int32_t tokens, int32_t top_k
 int32_t bsr_expert_scatter(const void* x_dev, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos_dev,
                            void* rows_dev_out, void* stream);
 /* The same with the rows in E4M3 blocks: codes_dev_out [tokens * top_k, dim] and scale_dev_out [tokens * top_k,
- * bsr_e4m3_scale_stride(dim)], as bsr_quantize_e4m3_rows128 would make them from the scattered rows.  dim a multiple of 16. */
+ * bsr_e4m3_scale_stride(dim)], as bsr_quantize_e4m3_rows128 would make them from the scattered rows.  dim a multiple of 16,
+ * tokens * ceil(dim / 128) < 2^32 - 2^16. */
 int32_t bsr_expert_scatter_e4m3(const void* x_dev, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos_dev,
                                 void* codes_dev_out, void* scale_dev_out, void* stream);
 
@@ -429,7 +430,8 @@ int32_t bsr_expert_combine_backward(const void* dout_dev, int32_t dtype, const v
                                     const float* weights_dev, void* drows_dev_out, float* dweights_dev_out, int32_t tokens, int32_t dim,
                                     int32_t top_k, void* stream);
 
-/* Rows x [m, k] in `dtype` to codes [m, k] and scales [m, bsr_e4m3_scale_stride(k)]; k a multiple of 16. */
+/* Rows x [m, k] in `dtype` to codes [m, k] and scales [m, bsr_e4m3_scale_stride(k)]; k a multiple of 16,
+ * m * ceil(k / 128) < 2^32 - 2^16. */
 int32_t bsr_quantize_e4m3_rows128(const void* x_dev, int32_t dtype, int32_t m, int32_t k, void* codes_dev_out, void* scale_dev_out, void* stream);
 /* Stacked weights w [count, n, k] in `dtype` to codes [count, n, k] and scales [count, ceil(n / 128), bsr_e4m3_scale_stride(k)].  With
  * codes_t_dev_out (then scale_t_dev_out too; else both NULL) also the transposed copies [count, k, n] with scales [count,

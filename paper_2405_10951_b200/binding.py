@@ -298,16 +298,20 @@ def bsr_attention_backward(qkv, dout, lse, score_grad=None, use_tensor_cores: bo
 # ---- rows of an expert layer, products in 8-bit blocks of 128 -----------------------------------
 # Outputs may be passed in (a decoding loop or a captured graph keeps its buffers); what is not is allocated.  The library sees
 # pointers alone, so types, shapes, contiguity and devices are checked here.
-def _same_device(*tensors):
+# A call's checks cost about as much as a small kernel runs, so they are written for few interpreter steps: shapes are compared as
+# tuples, devices as ordinals, and messages are made on refusal only.
+def _run_on(*tensors):
+    """The current stream of the current device, on which all tensors have to be."""
     import torch
-    device = torch.device("cuda", torch.cuda.current_device())
+    ordinal = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device != device:
-            raise BsrError(-1, f"tensor on {t.device}: the call runs on the current device, {device}")
+        if t is not None and t.get_device() != ordinal:
+            raise BsrError(-1, f"tensor on {t.device}: the call runs on the current device, cuda:{ordinal}")
+    return torch._C._cuda_getCurrentRawStream(ordinal)
 
 
 def _takes(name, t, dtypes, shape):
-    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype not in dtypes or t.shape != shape or not t.is_contiguous():
         raise BsrError(-1, f"{name} must be a contiguous tensor of {' or '.join(map(str, dtypes))} and shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
@@ -341,8 +345,8 @@ def bsr_expert_sort(expert, experts: int, pos=None, seg_start=None):
         seg_start = torch.empty(max(experts, 0) + 1, dtype=torch.int32, device=expert.device)
     _takes("pos", pos, (torch.int32,), (tokens, top_k))
     _takes("seg_start", seg_start, (torch.int32,), (experts + 1,))
-    _same_device(expert, pos, seg_start)
-    _check(lib().bsr_expert_sort(_at(expert), tokens, top_k, experts, _at(pos), _at(seg_start), _stream()))
+    stream = _run_on(expert, pos, seg_start)
+    _check(lib().bsr_expert_sort(_at(expert), tokens, top_k, experts, _at(pos), _at(seg_start), stream))
     return pos, seg_start
 
 
@@ -357,8 +361,8 @@ def bsr_expert_scatter(x, pos, rows=None):
     _takes("x", x, (x.dtype,), (tokens, dim))
     _takes("pos", pos, (torch.int32,), (tokens, top_k))
     _takes("rows", rows, (x.dtype,), (tokens * top_k, dim))
-    _same_device(x, pos, rows)
-    _check(lib().bsr_expert_scatter(_at(x), dt, tokens, dim, top_k, _at(pos), _at(rows), _stream()))
+    stream = _run_on(x, pos, rows)
+    _check(lib().bsr_expert_scatter(_at(x), dt, tokens, dim, top_k, _at(pos), _at(rows), stream))
     return rows
 
 
@@ -371,8 +375,8 @@ def bsr_expert_scatter_e4m3(x, pos, q=None, scale=None):
     q, scale = _codes_out(x, (tokens * top_k, dim), q, scale)
     _takes("x", x, (x.dtype,), (tokens, dim))
     _takes("pos", pos, (torch.int32,), (tokens, top_k))
-    _same_device(x, pos, q, scale)
-    _check(lib().bsr_expert_scatter_e4m3(_at(x), dt, tokens, dim, top_k, _at(pos), _at(q), _at(scale), _stream()))
+    stream = _run_on(x, pos, q, scale)
+    _check(lib().bsr_expert_scatter_e4m3(_at(x), dt, tokens, dim, top_k, _at(pos), _at(q), _at(scale), stream))
     return q, scale
 
 
@@ -392,8 +396,8 @@ def bsr_expert_combine(rows, pos, weights=None, residual=None, out=None, dtype=N
         _takes("weights", weights, (torch.float32,), (tokens, top_k))
     if residual is not None:
         _takes("residual", residual, (out.dtype,), (tokens, dim))
-    _same_device(rows, pos, weights, residual, out)
-    _check(lib().bsr_expert_combine(_at(rows), rt, _at(pos), _at(weights), _at(residual), _at(out), ot, tokens, dim, top_k, _stream()))
+    stream = _run_on(rows, pos, weights, residual, out)
+    _check(lib().bsr_expert_combine(_at(rows), rt, _at(pos), _at(weights), _at(residual), _at(out), ot, tokens, dim, top_k, stream))
     return out
 
 
@@ -413,8 +417,8 @@ def bsr_expert_combine_backward(dout, rows, pos, weights, drows=None, dw=None):
     _takes("weights", weights, (torch.float32,), (tokens, top_k))
     _takes("drows", drows, (rows.dtype,), (tokens * top_k, dim))
     _takes("dw", dw, (torch.float32,), (tokens, top_k))
-    _same_device(dout, rows, pos, weights, drows, dw)
-    _check(lib().bsr_expert_combine_backward(_at(dout), ot, _at(rows), rt, _at(pos), _at(weights), _at(drows), _at(dw), tokens, dim, top_k, _stream()))
+    stream = _run_on(dout, rows, pos, weights, drows, dw)
+    _check(lib().bsr_expert_combine_backward(_at(dout), ot, _at(rows), rt, _at(pos), _at(weights), _at(drows), _at(dw), tokens, dim, top_k, stream))
     return drows, dw
 
 
@@ -442,8 +446,8 @@ def bsr_quantize_e4m3_rows128(x, q=None, scale=None):
     dt = _float_type("x", x)
     q, scale = _codes_out(x, (m, k), q, scale)
     _takes("x", x, (x.dtype,), (m, k))
-    _same_device(x, q, scale)
-    _check(lib().bsr_quantize_e4m3_rows128(_at(x), dt, m, k, _at(q), _at(scale), _stream()))
+    stream = _run_on(x, q, scale)
+    _check(lib().bsr_quantize_e4m3_rows128(_at(x), dt, m, k, _at(q), _at(scale), stream))
     return q, scale
 
 
@@ -471,8 +475,8 @@ def bsr_quantize_e4m3_blocks128(w, transposed: bool = False, q=None, scale=None,
     q, scale = outputs(q, scale, n, k)
     if transposed or qt is not None or scale_t is not None:
         qt, scale_t = outputs(qt, scale_t, k, n, "_t")
-    _same_device(w, q, scale, qt, scale_t)
-    _check(lib().bsr_quantize_e4m3_blocks128(_at(w), dt, stack[0] if stack else 1, n, k, _at(q), _at(scale), _at(qt), _at(scale_t), _stream()))
+    stream = _run_on(w, q, scale, qt, scale_t)
+    _check(lib().bsr_quantize_e4m3_blocks128(_at(w), dt, stack[0] if stack else 1, n, k, _at(q), _at(scale), _at(qt), _at(scale_t), stream))
     return (q, scale) if qt is None else (q, scale, qt, scale_t)
 
 
@@ -499,8 +503,8 @@ def bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, bias=None, act: int = ACT_N
     """y [m, n] bf16 = act(x W^T + bias) from the codes and scales of x [m, k] and W [n, k].  act ACT_GELU: the pre-activation goes to z
     [m, n] bf16 if that is given; ACT_GELU_GRAD: the product is multiplied by GELU'(z)."""
     m, n, k, y = _block128_operands(xq, xs, wq, ws, (), bias, act, z, y)
-    _same_device(xq, xs, wq, ws, bias, z, y)
-    _check(lib().bsr_linear_forward_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(z), _at(y), m, n, k, act, _stream()))
+    stream = _run_on(xq, xs, wq, ws, bias, z, y)
+    _check(lib().bsr_linear_forward_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(z), _at(y), m, n, k, act, stream))
     return y
 
 
@@ -511,8 +515,8 @@ def bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg_start, bias=None, act: i
     experts = wq.shape[0]
     m, n, k, y = _block128_operands(xq, xs, wq, ws, (experts,), bias, act, z, y)
     _takes("seg_start", seg_start, (torch.int32,), (experts + 1,))
-    _same_device(xq, xs, wq, ws, seg_start, bias, z, y)
-    _check(lib().bsr_expert_linear_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(seg_start), _at(z), _at(y), m, n, k, experts, act, _stream()))
+    stream = _run_on(xq, xs, wq, ws, seg_start, bias, z, y)
+    _check(lib().bsr_expert_linear_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(seg_start), _at(z), _at(y), m, n, k, experts, act, stream))
     return y
 
 

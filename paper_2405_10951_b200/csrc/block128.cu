@@ -12,42 +12,58 @@
 
 namespace bsr {
 
-// Rows of x to codes and scales, a warp per 512 values of a row: a lane has 16 of them, eight lanes a block, and the four blocks'
-// bytes make one word of scales.  With `pos`, token t's codes go to the rows pos[t, 0 .. top_k) (negative: none) of what is
-// written, which has `rows` of them; without it to row t.
-template <typename T, bool SCATTER>
-__global__ void __launch_bounds__(256)
-quantize_rows128_kernel(const T* __restrict__ x, int m, int k, int groups, const int* __restrict__ pos, int top_k, unsigned rows,
-                        uint8_t* __restrict__ q, uint32_t* __restrict__ scale) {
+// Rows of x to codes and scales, eight lanes a block of 128, 16 values each.  A thread has the loads of U blocks on their way (loads in
+// flight are what the bandwidth hangs on).  The group of a row's last block also writes the padding behind its scales.  With
+// `pos`, token t's codes go to the rows pos[t, 0 .. top_k) (negative: none) of what is written, which has `rows` of them; without
+// it to row t.
+constexpr int QR_THREADS = 256, QR_UNITS = QR_THREADS / 8;
+template <typename T, bool SCATTER, int U>
+__global__ void __launch_bounds__(QR_THREADS)
+quantize_rows128_kernel(const T* __restrict__ x, unsigned units, int k, unsigned kblocks, int stride, const int* __restrict__ pos, int top_k, unsigned rows,
+                        uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
   dependent_sync();
-  const long unit = ((long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  if (unit >= (long)m * groups) return;
-  const int row = (int)(unit / groups), g = (int)(unit - (long)row * groups), col = g * 512 + lane * 16;
-  Codes16 c;
-  float v[16];
-  if (col < k) load_values16(x + (size_t)row * k + col, v);
-  else {
+  const unsigned u0 = blockIdx.x * (QR_UNITS * U) + (threadIdx.x >> 3);
+  const int lane8 = threadIdx.x & 7;
+  Values16<T> v[U];
+  unsigned row[U], blk[U];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = 0.f;
+  for (int i = 0; i < U; ++i) {
+    const unsigned u = u0 + i * QR_UNITS;
+    row[i] = u / kblocks;
+    blk[i] = u - row[i] * kblocks;
+    const int col = (int)blk[i] * 128 + lane8 * 16;
+    if (u < units && col < k) v[i].load(x + (size_t)row[i] * k + col);
+    else v[i].zero();
   }
-  uint32_t top = finite_max16(v);
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const uint32_t byte = scale_byte(top);
-  c = codes16(v, byte);
-  const uint32_t word = __shfl_sync(0xffffffffu, byte, 0) | __shfl_sync(0xffffffffu, byte, 8) << 8 | __shfl_sync(0xffffffffu, byte, 16) << 16 |
-                        __shfl_sync(0xffffffffu, byte, 24) << 24;
-  if constexpr (SCATTER) {
-    for (int s = 0; s < top_k; ++s) {
-      const unsigned to = (unsigned)pos[(size_t)row * top_k + s];
-      if (to >= rows) continue;
-      if (col < k) *reinterpret_cast<uint4*>(q + (size_t)to * k + col) = c.u;
-      if (lane == 0) scale[(size_t)to * groups + g] = word;
+  for (int i = 0; i < U; ++i) {
+    uint32_t top = v[i].top();
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const bool finite = top < F32_INF;
+    if (!__all_sync(0xffffffffu, finite)) {
+      uint32_t f = finite_top(v[i]);
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) f = max(f, __shfl_xor_sync(0xffffffffu, f, o));
+      top = f;
     }
-  } else {
-    if (col < k) *reinterpret_cast<uint4*>(q + (size_t)row * k + col) = c.u;
-    if (lane == 0) scale[(size_t)row * groups + g] = word;
+    const uint32_t byte = scale_byte(top);
+    const uint4 c = codes16(v[i], byte, finite);
+    const int col = (int)blk[i] * 128 + lane8 * 16;
+    if (u0 + i * QR_UNITS >= units) continue;
+    const int pad = blk[i] == kblocks - 1 ? stride - (int)kblocks : 0;           // lane 0 writes the scale, lanes 1 .. 3 the padding
+    auto put = [&](size_t to) {
+      if (col < k) *reinterpret_cast<uint4*>(q + to * k + col) = c;
+      if (lane8 <= pad) scale[to * stride + blk[i] + lane8] = (uint8_t)(lane8 == 0 ? byte : 127u);
+    };
+    if constexpr (SCATTER) {
+      for (int s = 0; s < top_k; ++s) {
+        const unsigned to = (unsigned)pos[(size_t)row[i] * top_k + s];
+        if (to < rows) put(to);
+      }
+    } else {
+      put(row[i]);
+    }
   }
 }
 
@@ -67,34 +83,41 @@ quantize_blocks128_kernel(const T* __restrict__ w, int n, int k, uint8_t* __rest
   const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 16, col = kb * 128 + c0;
   w += mat * n * k;
   q += mat * n * k;
-  float v[4][16];
+  Values16<T> v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = nb * 128 + r0 + 32 * i;
-    if (row < n && col < k) load_values16(w + (size_t)row * k + col, v[i]);
-    else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) v[i][j] = 0.f;
-    }
+    if (row < n && col < k) v[i].load(w + (size_t)row * k + col);
+    else v[i].zero();
   }
   uint32_t top = 0;
+  auto reduce = [&]() {
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) top = max(top, finite_max16(v[i]));
-  top = __reduce_max_sync(0xffffffffu, top);
-  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
-  __syncthreads();
+    for (int i = 0; i < QB_THREADS / 32; ++i) top = max(top, tops[i]);
+  };
 #pragma unroll
-  for (int i = 0; i < QB_THREADS / 32; ++i) top = max(top, tops[i]);
+  for (int i = 0; i < 4; ++i) top = max(top, v[i].top());
+  reduce();
+  const bool finite = top < F32_INF;
+  if (!finite) {                                 // (the same for all threads)
+    __syncthreads();
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, finite_top(v[i]));
+    reduce();
+  }
   const uint32_t byte = scale_byte(top);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = r0 + 32 * i, row = nb * 128 + r;
-    const Codes16 c = codes16(v[i], byte);
-    if (row < n && col < k) *reinterpret_cast<uint4*>(q + (size_t)row * k + col) = c.u;
+    const uint4 c = codes16(v[i], byte, finite);
+    if (row < n && col < k) *reinterpret_cast<uint4*>(q + (size_t)row * k + col) = c;
     if (qt != nullptr) {
-      const uint32_t* u = reinterpret_cast<const uint32_t*>(&c.u);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) tile[r * 33 + c0 / 4 + j] = u[j];
+      uint32_t* at = tile + r * 33 + c0 / 4;
+      at[0] = c.x; at[1] = c.y; at[2] = c.z; at[3] = c.w;
     }
   }
   // scales: the thread of the block's first column writes its byte, the last block's threads the padding behind it
@@ -144,13 +167,15 @@ int scale_stride128(int k) { return (k + 511) / 512 * 4; }
 
 template <typename T>
 static void quantize_rows(const Ctx& c, const void* x, int m, int k, const int* pos, int top_k, void* q, void* scale) {
-  const int groups = scale_stride128(k) / 4;
-  const long blocks = ((long)m * groups + 7) / 8;
+  const unsigned kblocks = (unsigned)ceil_div(k, 128), units = (unsigned)m * kblocks;
+  const int stride = scale_stride128(k);
+  constexpr int U = sizeof(T) == 2 ? 2 : 1;
+  const unsigned per = QR_UNITS * U, blocks = (units + per - 1) / per;
   note_launch(1);
   if (pos != nullptr)
-    launch_k(quantize_rows128_kernel<T, true>, (unsigned)blocks, 256, 0, c.stream, (const T*)x, m, k, groups, pos, top_k, (unsigned)m * (unsigned)top_k, (uint8_t*)q, (uint32_t*)scale);
+    launch_k(quantize_rows128_kernel<T, true, U>, blocks, QR_THREADS, 0, c.stream, (const T*)x, units, k, kblocks, stride, pos, top_k, (unsigned)m * (unsigned)top_k, (uint8_t*)q, (uint8_t*)scale);
   else
-    launch_k(quantize_rows128_kernel<T, false>, (unsigned)blocks, 256, 0, c.stream, (const T*)x, m, k, groups, pos, top_k, 0u, (uint8_t*)q, (uint32_t*)scale);
+    launch_k(quantize_rows128_kernel<T, false, U>, blocks, QR_THREADS, 0, c.stream, (const T*)x, units, k, kblocks, stride, pos, top_k, 0u, (uint8_t*)q, (uint8_t*)scale);
 }
 
 void quantize_rows128(const Ctx& c, const void* x, int m, int k, const int* pos, int top_k, void* q, void* scale) {

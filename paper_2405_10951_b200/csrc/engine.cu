@@ -1801,6 +1801,9 @@ static int check_slots(int32_t tokens, int32_t dim, int32_t top_k, int32_t dtype
   return BSR_OK;
 }
 
+// The kernels number blocks of 128 with 32 bits.
+static bool few_blocks(int64_t m, int64_t k) { return m * ((k + 127) / 128) < (int64_t)UINT32_MAX - 65535; }
+
 int32_t bsr_e4m3_scale_stride(int32_t k) { return k < 1 ? 0 : scale_stride128(k); }
 
 int32_t bsr_expert_sort(const int32_t* expert, int32_t tokens, int32_t top_k, int32_t experts, int32_t* pos, int32_t* seg_start, void* stream) {
@@ -1826,7 +1829,7 @@ int32_t bsr_expert_scatter_e4m3(const void* x, int32_t dtype, int32_t tokens, in
                                 void* scale, void* stream) {
   if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
   if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
-  if (dim % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "dim must be a multiple of 16");
+  if (dim % 16 != 0 || !few_blocks(tokens, dim)) return set_err(g_error, BSR_ERR_INVALID_ARG, "need dim a multiple of 16 and tokens * ceil(dim / 128) < 2^32 - 2^16");
   if (tokens == 0) return BSR_OK;
   if (x == nullptr || pos == nullptr || codes == nullptr || scale == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   if (unaligned({x, codes}) || unaligned({scale}, 4)) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned, scales 4-byte");
@@ -1860,7 +1863,7 @@ int32_t bsr_expert_combine_backward(const void* dout, int32_t dtype, const void*
 
 int32_t bsr_quantize_e4m3_rows128(const void* x, int32_t dtype, int32_t m, int32_t k, void* codes, void* scale, void* stream) {
   if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
-  if (m < 0 || k < 16 || k % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0 and k a multiple of 16");
+  if (m < 0 || k < 16 || k % 16 != 0 || !few_blocks(m, k)) return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0, k a multiple of 16 and m * ceil(k / 128) < 2^32 - 2^16");
   if (m == 0) return BSR_OK;
   if (x == nullptr || codes == nullptr || scale == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   if (unaligned({x, codes}) || unaligned({scale}, 4)) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned, scales 4-byte");

@@ -4,6 +4,8 @@
 // All sums run in slot order: results do not depend on scheduling.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "kernels.h"
 
@@ -13,12 +15,14 @@ namespace cg = cooperative_groups;
 
 // ---- positions ---------------------------------------------------------------------------------------------------------
 // A stable counting sort in one launch: every warp has a run of consecutive slots.  It counts its run per expert in a row of
-// shared memory of its own (lanes with equal experts find each other by match, so one of them adds for all); the counts become
-// starts, down the warps, over the CTAs of the cluster through distributed shared memory, and along the experts; then the warp walks its
-// run again and hands out positions.  Bound by latency: the bytes are 8 a slot.
-constexpr int SORT_CLUSTER = 8, SORT_MAX_E = 1024;
+// shared memory of its own; the counts become starts, down the warps, over the CTAs of the cluster through distributed shared memory, and
+// along the experts; then the warp walks its run again and hands out positions: lanes with equal experts find each other by
+// a ballot for each bit of the expert's number (with the match instruction 262144 slots of 128 experts took 57 us, so 24, and 13.7 with
+// sixteen CTAs instead of eight).  Bound by latency (the bytes are 8 a slot), so the experts' numbers of four steps are
+// loaded at once.
+constexpr int SORT_CLUSTER = 16, SORT_U = 4;
 
-template <int THREADS>
+template <int THREADS, int BITS>
 __global__ void __launch_bounds__(THREADS)
 expert_sort_kernel(const int* __restrict__ expert, int slots, int E, int per_warp, int* __restrict__ pos, int* __restrict__ seg_start) {
   constexpr int W = THREADS / 32;
@@ -26,29 +30,37 @@ expert_sort_kernel(const int* __restrict__ expert, int slots, int E, int per_war
   int* hist = sort_smem;                       // [W][E]
   int* total = hist + W * E;                   // [E], read by the cluster
   int* start = total + E;                      // [E]
-  __shared__ int carry[W + 1];
+  __shared__ int carry[W];
   cg::cluster_group cluster = cg::this_cluster();
   const int ranks = cluster.num_blocks(), rank = cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t lt = (1u << lane) - 1u;
-  for (int i = threadIdx.x; i < W * E; i += THREADS) hist[i] = 0;
-  dependent_sync();
-  __syncthreads();
   int* mine = hist + warp * E;
+  for (int i = lane; i < E; i += 32) mine[i] = 0;
+  __syncwarp();
+  dependent_sync();
   const long first = (long)(rank * W + warp) * per_warp;
   const int begin = (int)min(first, (long)slots), end = (int)min(first + per_warp, (long)slots);
-  for (int i0 = begin; i0 < end; i0 += 32) {
-    const int i = i0 + lane;
-    const int e = i < end ? expert[i] : -1;
-    const bool has = e >= 0 && e < E;
-    const uint32_t same = __match_any_sync(0xffffffffu, has ? e : -1);
-    if (has && (same & lt) == 0) mine[e] += __popc(same);
-    __syncwarp();
+  auto load = [&](int i0, int* e) {            // -1: no expert
+#pragma unroll
+    for (int u = 0; u < SORT_U; ++u) {
+      const int i = i0 + u * 32 + lane;
+      e[u] = i < end ? expert[i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < SORT_U; ++u) e[u] = e[u] < E ? max(e[u], -1) : -1;
+  };
+  for (int i0 = begin; i0 < end; i0 += 32 * SORT_U) {
+    int e[SORT_U];
+    load(i0, e);
+#pragma unroll
+    for (int u = 0; u < SORT_U; ++u)
+      if (e[u] >= 0) atomicAdd(&mine[e[u]], 1);         // integer counts: order-independent
   }
   __syncthreads();
   for (int e = threadIdx.x; e < E; e += THREADS) {
     int s = 0;
-#pragma unroll
+#pragma unroll 8
     for (int w = 0; w < W; ++w) {
       const int n = hist[w * E + e];
       hist[w * E + e] = s;
@@ -56,17 +68,21 @@ expert_sort_kernel(const int* __restrict__ expert, int slots, int E, int per_war
     }
     total[e] = s;
   }
-  cluster.sync();
+  if (ranks > 1) cluster.sync(); else __syncthreads();
   // starts of the experts' segments (an exclusive scan over all experts) and of this CTA's part of each
   int below = 0;
   for (int e0 = 0; e0 < E; e0 += THREADS) {
     const int e = e0 + threadIdx.x;
     int all = 0, before = 0;
     if (e < E) {
-      for (int r = 0; r < ranks; ++r) {
-        const int n = *cluster.map_shared_rank(&total[e], r);
-        all += n;
-        if (r < rank) before += n;
+      if (ranks == 1) all = total[e];
+      else {
+#pragma unroll
+        for (int r = 0; r < SORT_CLUSTER; ++r) {
+          const int n = r < ranks ? *cluster.map_shared_rank(&total[e], r) : 0;
+          all += n;
+          if (r < rank) before += n;
+        }
       }
     }
     int scan = all;
@@ -77,12 +93,10 @@ expert_sort_kernel(const int* __restrict__ expert, int slots, int E, int per_war
     }
     if (lane == 31) carry[warp] = scan;
     __syncthreads();
-    int prior = below;
-    for (int w = 0; w < W; ++w) {
-      const int n = carry[w];
-      if (w < warp) prior += n;
-      below += n;
-    }
+    int prior = lane < W ? carry[lane] : 0;            // (at most 32 warps)
+    const int sum = warp_sum_int(prior);
+    prior = below + warp_sum_int(lane < warp ? prior : 0);
+    below += sum;
     if (e < E) {
       start[e] = prior + scan - all + before;
       if (rank == 0) seg_start[e] = prior + scan - all;
@@ -90,118 +104,187 @@ expert_sort_kernel(const int* __restrict__ expert, int slots, int E, int per_war
     __syncthreads();
   }
   if (rank == 0 && threadIdx.x == 0) seg_start[E] = below;
-  for (int i0 = begin; i0 < end; i0 += 32) {
-    const int i = i0 + lane;
-    const int e = i < end ? expert[i] : -1;
-    const bool has = e >= 0 && e < E;
-    const uint32_t same = __match_any_sync(0xffffffffu, has ? e : -1);
-    const int at = has ? start[e] + mine[e] + __popc(same & lt) : -1;
-    __syncwarp();
-    if (has && (same & lt) == 0) mine[e] += __popc(same);
-    __syncwarp();
-    if (i < end) pos[i] = at;
+  for (int i0 = begin; i0 < end; i0 += 32 * SORT_U) {
+    int e[SORT_U];
+    load(i0, e);
+#pragma unroll
+    for (int u = 0; u < SORT_U; ++u) {
+      const int i = i0 + u * 32 + lane;
+      uint32_t same = __ballot_sync(0xffffffffu, e[u] >= 0);
+#pragma unroll
+      for (int b = 0; b < BITS; ++b) {
+        const bool bit = (e[u] >> b) & 1;
+        same &= __ballot_sync(0xffffffffu, bit) ^ (bit ? 0u : 0xffffffffu);
+      }
+      int at = -1;
+      if (e[u] >= 0) {
+        at = start[e[u]] + mine[e[u]] + __popc(same & lt);
+      }
+      __syncwarp();
+      if (e[u] >= 0 && (same & lt) == 0) mine[e[u]] += __popc(same);
+      __syncwarp();
+      if (i < end) pos[i] = at;
+    }
   }
-  cluster.sync();                              // no CTA leaves while another may still read its counts
+  if (ranks > 1) cluster.sync();               // no CTA leaves while another may still read its counts
 }
 
 // ---- rows --------------------------------------------------------------------------------------------------------------
-// rows[pos[t, s]] = x[t], 16 bytes a lane: x is read once, whatever the number of slots.  A warp has `cols` chunks of a token.
+// rows[pos[t, s]] = x[t], 16 bytes a thread: x is read once, whatever the number of slots.  A CTA has `cx` chunks of `ty` tokens beside
+// one another, so that a row's bytes leave together (32768 tokens, 8 slots, 2048 wide: a warp walking a token's row 191 us, this
+// 176, the loads of two tokens a thread 180).
 __global__ void __launch_bounds__(256)
-expert_scatter_kernel(const uint4* __restrict__ x, int tokens, int chunks, int parts, int top_k, const int* __restrict__ pos, unsigned rows,
-                      uint4* __restrict__ out) {
+expert_scatter_kernel(const uint4* __restrict__ x, int tokens, int chunks, int cx, int ty, int top_k, const int* __restrict__ pos, unsigned rows, uint4* __restrict__ out) {
   dependent_sync();
-  const long unit = ((long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  if (unit >= (long)tokens * parts) return;
-  const int t = (int)(unit / parts), part = (int)(unit - (long)t * parts);
+  const int tl = threadIdx.x / cx, ch = blockIdx.y * cx + threadIdx.x - tl * cx, t = blockIdx.x * ty + tl;
+  if (tl >= ty || ch >= chunks || t >= tokens) return;
+  const uint4 v = x[(size_t)t * chunks + ch];
   const int* p = pos + (size_t)t * top_k;
-  for (int ch = part * 32 + lane; ch < chunks; ch += parts * 32) {
-    const uint4 v = x[(size_t)t * chunks + ch];
-    for (int s = 0; s < top_k; ++s) {
-      const unsigned to = (unsigned)p[s];
-      if (to < rows) out[(size_t)to * chunks + ch] = v;
-    }
+#pragma unroll 4
+  for (int s = 0; s < top_k; ++s) {
+    const unsigned to = (unsigned)p[s];
+    if (to < rows) out[(size_t)to * chunks + ch] = v;
   }
 }
 
-// out[t] = residual[t] + sum_s w[t, s] rows[pos[t, s]] (without w: the plain sum, the gradient of the scatter).  N values a lane.
-template <typename TR, typename TO, int N>
+// 16 bytes of a row and the values in them (eight bf16, four floats).
+template <typename T> struct Chunk { static constexpr int N = 16 / sizeof(T); };
+template <typename T> __device__ __forceinline__ void chunk_values(const uint4& u, float* v);
+template <> __device__ __forceinline__ void chunk_values<float>(const uint4& u, float* v) {
+  v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+}
+template <> __device__ __forceinline__ void chunk_values<bf16>(const uint4& u, float* v) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+}
+// As many values of the other tensor's row, whatever its type.
+template <int N> __device__ __forceinline__ void load_vals(const float* p, float* f) { load_n<N>(p, f); }
+template <int N> __device__ __forceinline__ void load_vals(const bf16* p, float* f) { if constexpr (N == 8) load16(p, f); else load4(p, f); }
+template <int N> __device__ __forceinline__ void store_vals(float* p, const float* f) { store_n<N>(p, f); }
+template <int N> __device__ __forceinline__ void store_vals(bf16* p, const float* f) { if constexpr (N == 8) store16(p, f); else store4(p, f); }
+
+// out[t] = residual[t] + sum_s w[t, s] rows[pos[t, s]] (without w: the plain sum, the gradient of the scatter).
+// Bytes bound it, and what moves them is loads in flight: rows lie anywhere, so a thread reads the positions of S slots, then has their
+// S loads of 16 bytes on their way.  More a thread (eight slots, or several tokens) leaves fewer threads on an SM and is slower:
+// 12608 tokens, 2 slots, 384 wide 14.5 us with four tokens a thread, 11.2 with one; 32768 tokens, 8 slots, 2048 wide 242 us with
+// eight slots at once, 219 with four.
+template <typename TR, typename TO, int S>
 __global__ void __launch_bounds__(256)
 expert_combine_kernel(const TR* __restrict__ rows, const int* __restrict__ pos, const float* __restrict__ w, const TO* __restrict__ residual,
-                      TO* __restrict__ out, int tokens, int dim, int parts, int top_k, unsigned nrows) {
+                      TO* __restrict__ out, int tokens, int dim, int cx, int ty, int top_k, unsigned nrows) {
+  constexpr int N = Chunk<TR>::N;
   dependent_sync();
-  const long unit = ((long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  if (unit >= (long)tokens * parts) return;
-  const int t = (int)(unit / parts), part = (int)(unit - (long)t * parts);
-  const int* p = pos + (size_t)t * top_k;
-  for (int col = (part * 32 + lane) * N; col < dim; col += parts * 32 * N) {
-    float acc[N];
-    if (residual != nullptr) load_n<N>(residual + (size_t)t * dim + col, acc);
-    else {
+  const int tl = threadIdx.x / cx, col = (blockIdx.y * cx + threadIdx.x - tl * cx) * N, t = blockIdx.x * ty + tl;
+  if (tl >= ty || col >= dim || t >= tokens) return;
+  float acc[N];
+  if (residual != nullptr) load_vals<N>(residual + (size_t)t * dim + col, acc);
+  else {
 #pragma unroll
-      for (int j = 0; j < N; ++j) acc[j] = 0.f;
-    }
-    for (int s0 = 0; s0 < top_k; s0 += 4) {
-      float v[4][N], ws[4];
-      bool has[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const unsigned from = s0 + u < top_k ? (unsigned)p[s0 + u] : 0xffffffffu;
-        has[u] = from < nrows;
-        ws[u] = w != nullptr && has[u] ? w[(size_t)t * top_k + s0 + u] : 1.f;
-        if (has[u]) load_n<N>(rows + (size_t)from * dim + col, v[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (has[u])
-#pragma unroll
-          for (int j = 0; j < N; ++j) acc[j] = fmaf(ws[u], v[u][j], acc[j]);
-    }
-    store_n<N>(out + (size_t)t * dim + col, acc);
+    for (int j = 0; j < N; ++j) acc[j] = 0.f;
   }
+  for (int s0 = 0; s0 < top_k; s0 += S) {
+    unsigned from[S];
+    uint4 v[S];
+    float ws[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const size_t slot = (size_t)t * top_k + s0 + s;
+      const bool is = s0 + s < top_k;
+      from[s] = is ? (unsigned)pos[slot] : 0xffffffffu;
+      ws[s] = is && w != nullptr ? w[slot] : 1.f;
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (from[s] < nrows) v[s] = *reinterpret_cast<const uint4*>(rows + (size_t)from[s] * dim + col);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (from[s] < nrows) {
+        float f[N];
+        chunk_values<TR>(v[s], f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] = fmaf(ws[s], f[j], acc[j]);
+      }
+  }
+  store_vals<N>(out + (size_t)t * dim + col, acc);
 }
 
-// drows[pos[t, s]] = w[t, s] dout[t];  dw[t, s] = <dout[t], rows[pos[t, s]]> (0 without an expert).  A warp a token, S slots at a time.
-template <typename TR, typename TO, int N, int S>
+// Sums of S values over the warp: each exchange halves the values that a lane still has, so that lanes s * 32 / S ... have the sum of
+// value s (S - 1 + log2(32 / S) shuffles instead of 5 S).  Returns this lane's.
+template <int S>
+__device__ __forceinline__ float warp_sums(float* v) {
+  const int lane = threadIdx.x & 31;
+  int o = 16;
+#pragma unroll
+  for (int n = S / 2; n > 0; n >>= 1, o >>= 1)
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const bool up = (lane & o) != 0;
+      const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  float s = v[0];
+  for (; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+
+// drows[pos[t, s]] = w[t, s] dout[t];  dw[t, s] = <dout[t], rows[pos[t, s]]> (0 without an expert).  `wpt` warps a token, by the length of
+// its row, S slots at a time with all their loads in flight; the warps' parts of a dot product meet in shared memory, in warp order.
+template <typename TR, typename TO, int S>
 __global__ void __launch_bounds__(256)
 expert_combine_bwd_kernel(const TO* __restrict__ dout, const TR* __restrict__ rows, const int* __restrict__ pos, const float* __restrict__ w,
-                          TR* __restrict__ drows, float* __restrict__ dw, int tokens, int dim, int top_k, unsigned nrows) {
+                          TR* __restrict__ drows, float* __restrict__ dw, int tokens, int dim, int wpt, int top_k, unsigned nrows) {
+  constexpr int N = Chunk<TR>::N, PER = 32 / S;
+  __shared__ float part[8][S];
   dependent_sync();
-  const int t = (int)(((long)blockIdx.x * blockDim.x + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-  if (t >= tokens) return;
-  const int* p = pos + (size_t)t * top_k;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tl = warp / wpt, wr = warp - tl * wpt;
+  const int t = blockIdx.x * (8 / wpt) + tl;
   for (int s0 = 0; s0 < top_k; s0 += S) {
     float dot[S], ws[S];
     unsigned at[S];
 #pragma unroll
-    for (int u = 0; u < S; ++u) {
-      at[u] = s0 + u < top_k ? (unsigned)p[s0 + u] : 0xffffffffu;
-      ws[u] = at[u] < nrows ? w[(size_t)t * top_k + s0 + u] : 0.f;
-      dot[u] = 0.f;
+    for (int s = 0; s < S; ++s) {
+      const bool is = t < tokens && s0 + s < top_k;
+      at[s] = is ? (unsigned)pos[(size_t)t * top_k + s0 + s] : 0xffffffffu;
+      ws[s] = is ? w[(size_t)t * top_k + s0 + s] : 0.f;
+      dot[s] = 0.f;
     }
-    for (int col = lane * N; col < dim; col += 32 * N) {
-      float g[N], v[S][N];
-      load_n<N>(dout + (size_t)t * dim + col, g);
+    if (t < tokens)
+      for (int col = (wr * 32 + lane) * N; col < dim; col += wpt * 32 * N) {
+        float g[N];
+        uint4 v[S];
+        load_vals<N>(dout + (size_t)t * dim + col, g);
 #pragma unroll
-      for (int u = 0; u < S; ++u)
-        if (at[u] < nrows) load_n<N>(rows + (size_t)at[u] * dim + col, v[u]);
+        for (int s = 0; s < S; ++s)
+          if (at[s] < nrows) v[s] = *reinterpret_cast<const uint4*>(rows + (size_t)at[s] * dim + col);
 #pragma unroll
-      for (int u = 0; u < S; ++u)
-        if (at[u] < nrows) {
-          float d[N];
+        for (int s = 0; s < S; ++s)
+          if (at[s] < nrows) {
+            float d[N], f[N];
+            chunk_values<TR>(v[s], f);
 #pragma unroll
-          for (int j = 0; j < N; ++j) {
-            dot[u] = fmaf(g[j], v[u][j], dot[u]);
-            d[j] = ws[u] * g[j];
+            for (int j = 0; j < N; ++j) {
+              dot[s] = fmaf(g[j], f[j], dot[s]);
+              d[j] = ws[s] * g[j];
+            }
+            store_vals<N>(drows + (size_t)at[s] * dim + col, d);
           }
-          store_n<N>(drows + (size_t)at[u] * dim + col, d);
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < S; ++u) {
-      const float sum = warp_sum(dot[u]);
-      if (lane == 0 && s0 + u < top_k) dw[(size_t)t * top_k + s0 + u] = at[u] < nrows ? sum : 0.f;
+      }
+    const float sum = warp_sums<S>(dot);
+    const int s = lane / PER;
+    const bool writes = lane % PER == 0 && t < tokens && s0 + s < top_k;
+    if (wpt == 1) {
+      if (writes) dw[(size_t)t * top_k + s0 + s] = sum;
+    } else {
+      if (lane % PER == 0) part[warp][s] = sum;
+      __syncthreads();
+      if (wr == 0 && writes) {
+        float all = sum;
+        for (int q = 1; q < wpt; ++q) all += part[warp + q][s];
+        dw[(size_t)t * top_k + s0 + s] = all;
+      }
+      __syncthreads();
     }
   }
 }
@@ -210,36 +293,51 @@ expert_combine_bwd_kernel(const TO* __restrict__ dout, const TR* __restrict__ ro
 // launchers
 // =================================================================================================
 int expert_sort(const Ctx& c, const int* expert, int slots, int E, int* pos, int* seg_start) {
-  constexpr int THREADS = 1024, W = THREADS / 32;
-  const int ranks = slots > W * 128 ? SORT_CLUSTER : 1;
-  const int per_warp = ceil_div(ceil_div(slots, ranks * W), 32) * 32;
-  const size_t smem = (size_t)(W + 2) * E * sizeof(int);
-  static SmemLimit lim;
-  if (!ensure_smem(lim, expert_sort_kernel<THREADS>, smem)) return -3;
-  note_launch(1);
-  launch_cluster(expert_sort_kernel<THREADS>, ranks, THREADS, smem, c.stream, ranks, expert, slots, E, per_warp, pos, seg_start);
-  return 0;
+  // Few slots (decoding) leave most of a large CTA idle, and its start takes longer: 4 slots, 16 experts 3.2 -> 2.4 us.  Many go to a
+  // cluster of sixteen CTAs, which the kernel has to be allowed once.
+  auto go = [&](auto kern, int threads, int ranks, SmemLimit& lim) {
+    const int warps = threads / 32, per_warp = ceil_div(ceil_div(slots, ranks * warps), 32) * 32;
+    const size_t smem = (size_t)(warps + 2) * E * sizeof(int);
+    if (!ensure_smem(lim, kern, smem)) return -3;
+    if (ranks > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return -3;
+    note_launch(1);
+    launch_cluster(kern, ranks, threads, smem, c.stream, ranks, expert, slots, E, per_warp, pos, seg_start);
+    return 0;
+  };
+  auto size = [&](auto bits) {
+    constexpr int B = decltype(bits)::value;
+    static SmemLimit small, large;
+    if (slots <= 2048) return go(expert_sort_kernel<256, B>, 256, 1, small);
+    const int want = ceil_div(slots, 4096);           // 128 slots a warp (25216 slots, 16 experts: 5.2 us; 512 a warp 9.8)
+    return go(expert_sort_kernel<1024, B>, 1024, want < SORT_CLUSTER ? want : SORT_CLUSTER, large);
+  };
+  return E <= 16 ? size(std::integral_constant<int, 4>()) : E <= 128 ? size(std::integral_constant<int, 7>()) : size(std::integral_constant<int, 10>());
 }
 
-// Warps a token: more than one where the tokens alone would leave SMs without work.
-static int parts_for(int tokens, int per_warp, int dim) {
-  const int most = ceil_div(dim, per_warp), want = ceil_div(B200_SMS * 16, tokens);
-  return most < want ? most : want;
-}
+// A row's chunks over the threads of a CTA: `cx` of them, `ty` tokens beside one another, a row of more than 256 in `parts`.
+struct Spread {
+  int parts, cx, ty, threads;
+  explicit Spread(int chunks) : parts(ceil_div(chunks, 256)), cx(ceil_div(chunks, parts)), ty(256 / cx), threads(ceil_div(cx * ty, 32) * 32) {}
+};
 
 void expert_scatter(const Ctx& c, const void* x, int tokens, int dim, int top_k, const int* pos, void* rows) {
-  const int chunks = (int)(dim * dtype_size(c.dtype) / 16), parts = parts_for(tokens, 32, chunks);
+  const int chunks = (int)(dim * dtype_size(c.dtype) / 16);
+  const Spread s(chunks);
   note_launch(1);
-  launch_k(expert_scatter_kernel, ceil_div((long)tokens * parts, 8), 256, 0, c.stream, (const uint4*)x, tokens, chunks, parts, top_k, pos, (unsigned)tokens * (unsigned)top_k, (uint4*)rows);
+  launch_k(expert_scatter_kernel, dim3(ceil_div(tokens, s.ty), s.parts), s.threads, 0, c.stream, (const uint4*)x, tokens, chunks, s.cx, s.ty, top_k, pos,
+           (unsigned)tokens * (unsigned)top_k, (uint4*)rows);
 }
 
 template <typename TR, typename TO>
 static void combine(const Ctx& c, const void* rows, const int* pos, const float* w, const void* residual, void* out, int tokens, int dim, int top_k) {
-  constexpr int N = sizeof(TR) + sizeof(TO) == 8 ? 4 : 8;
-  const int parts = parts_for(tokens, 32 * N, dim);
-  note_launch(1);
-  launch_k(expert_combine_kernel<TR, TO, N>, ceil_div((long)tokens * parts, 8), 256, 0, c.stream, (const TR*)rows, pos, w, (const TO*)residual, (TO*)out, tokens, dim, parts, top_k,
-           (unsigned)tokens * (unsigned)top_k);
+  const Spread s(dim / Chunk<TR>::N);
+  auto go = [&](auto kern) {
+    note_launch(1);
+    launch_k(kern, dim3(ceil_div(tokens, s.ty), s.parts), s.threads, 0, c.stream, (const TR*)rows, pos, w, (const TO*)residual, (TO*)out, tokens, dim, s.cx, s.ty, top_k,
+             (unsigned)tokens * (unsigned)top_k);
+  };
+  if (top_k <= 2) go(expert_combine_kernel<TR, TO, 2>);
+  else go(expert_combine_kernel<TR, TO, 4>);
 }
 
 void expert_combine(const Ctx& c, const void* rows, int rows_dtype, const int* pos, const float* w, const void* residual, void* out, int tokens, int dim, int top_k) {
@@ -249,13 +347,13 @@ void expert_combine(const Ctx& c, const void* rows, int rows_dtype, const int* p
 
 template <typename TR, typename TO>
 static void combine_bwd(const Ctx& c, const void* dout, const void* rows, const int* pos, const float* w, void* drows, float* dw, int tokens, int dim, int top_k) {
-  constexpr int N = sizeof(TR) + sizeof(TO) == 8 ? 4 : 8;
+  const int chunks = dim / Chunk<TR>::N, wpt = chunks <= 64 ? 1 : chunks <= 128 ? 2 : chunks <= 256 ? 4 : 8;
   auto go = [&](auto kern) {
     note_launch(1);
-    launch_k(kern, ceil_div((long)tokens, 8), 256, 0, c.stream, (const TO*)dout, (const TR*)rows, pos, w, (TR*)drows, dw, tokens, dim, top_k, (unsigned)tokens * (unsigned)top_k);
+    launch_k(kern, ceil_div(tokens, 8 / wpt), 256, 0, c.stream, (const TO*)dout, (const TR*)rows, pos, w, (TR*)drows, dw, tokens, dim, wpt, top_k, (unsigned)tokens * (unsigned)top_k);
   };
-  if (top_k <= 2) go(expert_combine_bwd_kernel<TR, TO, N, 2>);
-  else go(expert_combine_bwd_kernel<TR, TO, N, 4>);
+  if (top_k <= 2) go(expert_combine_bwd_kernel<TR, TO, 2>);
+  else go(expert_combine_bwd_kernel<TR, TO, 4>);         // (eight at once: 32768 tokens, 8 slots, 2048 wide 314 -> 354 us)
 }
 
 void expert_combine_bwd(const Ctx& c, const void* dout, const void* rows, int rows_dtype, const int* pos, const float* w, void* drows, float* dw, int tokens, int dim, int top_k) {

@@ -11,19 +11,24 @@
 // cost one copy of 512 bytes a 128 rows and four slabs.  (Scaling the partial sums of every slab in registers instead would read the
 // accumulators once a slab.)
 //
-// Persistent, one CTA per SM, tiles of 128 rows and 64, 128 or 192 columns (two accumulators of 192 leave tensor memory for
-// the scales; two of 256 would not):
+// Two kernels, both persistent, a tile's rows spread over warps in the same way:
+//   gemm_block128_kernel       one CTA a tile of 128 rows and 64, 128 or 192 columns (two accumulators of 192 leave tensor memory for
+//                              the scales; two of 256 would not)
+//   gemm_block128_pair_kernel  two CTAs (cta_group::2) a tile of 256 rows and up to 240 columns
 //   warp 0      : TMA producer (one lane)
 //   warp 1      : tensor-memory allocation, copies of scales to tensor memory, MMA issue (one lane)
 //   warp 2      : scales from global to shared memory, in the order in which tensor memory takes them
-//   warps 3..10 : epilogue, as in gemm_tc.cu
+//   warps 3..14 : epilogue, three warps per TMEM lane quarter
 // Every wait is bounded as in gemm_tc.cu.
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
 #include "tc_epilogue.cuh"
 #include "tc_ptx.cuh"
+#include "tc_pair.cuh"
 
 namespace bsr {
 namespace tcb {
@@ -31,14 +36,15 @@ using namespace tc;
 
 constexpr int BM = 128, BK = 128, UMMA_K = 32;             // a slab is a block of scales: 128 bytes of every row
 constexpr int A_BYTES = BM * BK;
-constexpr int RING_BYTES = 168 * 1024;
-constexpr int stages_for(int bn) { return RING_BYTES / (A_BYTES + bn * BK) < 8 ? RING_BYTES / (A_BYTES + bn * BK) : 8; }
-constexpr int SF_STAGES = 4, SF_BYTES = 3 * 512;           // words of 128 rows of A, of up to 256 rows of W
-constexpr int EPI_WARPS = 8, STAGING_BYTES = 32 * 128;
+constexpr int SF_BYTES = 3 * 512;                          // words of 128 rows of A, of up to 256 rows of W
+constexpr int EPI_WARPS = 12, EPI_SHARE = EPI_WARPS / 4;   // warps that share a quarter's chunks of columns
+// Scales wait in SF_STAGES stages of shared memory (their way there is long beside a group of few slabs) and go to tensor memory in turns
+// of two: the copy of a group's into the place of those before the last waits until the products that read these are done.
+constexpr int SF_STAGES = 4;
+constexpr int STAGING_BYTES = 4096;                        // a warp's 32 rows x 64 columns of bf16
 constexpr int THREADS = 96 + EPI_WARPS * 32;
 constexpr int MAX_E = 1024;
-constexpr int SMEM_BYTES = RING_BYTES + EPI_WARPS * STAGING_BYTES + SF_STAGES * SF_BYTES + 1024;
-constexpr uint32_t TMEM_COLS = 512, SF_COL = 384;          // four columns of A's scales and eight of W's per stage, 16 apart
+constexpr uint32_t TMEM_COLS = 512;
 
 // D = f32, A = W = E4M3 (format code 0), both along k, scales of type E8M0; sf is the byte of the scale words.
 __host__ __device__ constexpr uint32_t make_idesc_scaled(int m, int n) {
@@ -62,6 +68,30 @@ __device__ __forceinline__ uint64_t make_desc_scales(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
+// One lane of a converged warp, the same one every time.  What it issues to the tensor cores takes its operands from uniform registers only
+// where the compiler knows that a single lane runs: behind a comparison of the lane's number an MMA took 180 clocks to issue (whatever
+// its width), behind this none that shows.
+__device__ __forceinline__ bool elected() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
+}
+
+// Whether a phase is over, without waiting.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// The whole warp waits; false where any lane gave up.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abortp) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp)); }
+
 struct Problem {
   int M, N, K;                       // M: rows of A in all
   int tiles_n, experts;
@@ -70,42 +100,369 @@ struct Problem {
   const uint32_t* w_scale;           // [experts][ceil(N / 128)][groups]
 };
 
-// One tile.  r0 .. r1 - 1 are the rows that it stores.
-struct Tile { int r0, r1, nt, e; };
-__device__ __forceinline__ Tile decode_tile(int w, const Problem& p, const int* tile_start, const int* seg) {
+// What one tile covers: rows r0 .. r1 - 1 of expert e, columns from n0.
+struct Tile { int r0, r1, n0, e; };
+constexpr int LISTED = 32;
+struct Tables {
+  int tile_start[MAX_E + 1], seg[MAX_E + 1];
+  int warp_total[THREADS / 32];
+  Tile list[LISTED];                 // this worker's first tiles
+};
+__device__ __forceinline__ Tile find_tile(int w, const Problem& p, int rows, int width, const Tables& tab) {
   Tile t;
   const int mt = w / p.tiles_n;
-  t.nt = w - mt * p.tiles_n;
+  t.n0 = (w - mt * p.tiles_n) * width;
   if (p.seg_start == nullptr) {
     t.e = 0;
-    t.r0 = mt * BM;
-    t.r1 = min(p.M, t.r0 + BM);
+    t.r0 = mt * rows;
+    t.r1 = min(p.M, t.r0 + rows);
   } else {
     int lo = 0, hi = p.experts;      // the last expert whose first tile is not behind mt
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (tile_start[mid] <= mt) lo = mid; else hi = mid;
+      if (tab.tile_start[mid] <= mt) lo = mid; else hi = mid;
     }
     t.e = lo;
-    t.r0 = seg[lo] + (mt - tile_start[lo]) * BM;
-    t.r1 = min(seg[lo + 1], t.r0 + BM);
+    t.r0 = tab.seg[lo] + (mt - tab.tile_start[lo]) * rows;
+    t.r1 = min(tab.seg[lo + 1], t.r0 + rows);
   }
   return t;
 }
+// The tiles of one worker, ascending, columns fastest.  Four roles walk them: the first ones come from a list that the CTA's threads make
+// side by side.
+struct Walk {
+  int i, w, workers, items;
+  __device__ __forceinline__ Walk(int worker, int workers_, int items_) : i(0), w(worker), workers(workers_), items(items_) {}
+  __device__ __forceinline__ bool next(Tile& t, const Problem& p, int rows, int width, const Tables& tab) {
+    if (w >= items) return false;
+    t = i < LISTED ? tab.list[i] : find_tile(w, p, rows, width, tab);
+    ++i;
+    w += workers;
+    return true;
+  }
+};
+// All threads: segments, the first tile of every expert (tiles of `rows` rows) and the worker's list to shared memory; returns the number
+// of tiles.  Segments are cut to the rows there are, and one that reaches into a later one to what is before that, so that no row has two.
+__device__ __forceinline__ int make_tables(const Problem& p, int rows, int width, int worker, int workers, Tables& tab) {
+  int tiles_m = (p.M + rows - 1) / rows;
+  if (p.seg_start != nullptr) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i <= p.experts; i += THREADS) tab.seg[i] = min(max(p.seg_start[i], 0), p.M);
+    __syncthreads();
+    int falls = 0;
+    for (int i = threadIdx.x; i < p.experts; i += THREADS) falls |= tab.seg[i + 1] < tab.seg[i];
+    if (__syncthreads_or(falls)) {
+      if (threadIdx.x == 0)
+        for (int i = p.experts - 1; i >= 0; --i) tab.seg[i] = min(tab.seg[i], tab.seg[i + 1]);
+      __syncthreads();
+    }
+    int below = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += THREADS) {
+      const int e = e0 + threadIdx.x;
+      const int n = e < p.experts ? (tab.seg[e + 1] - tab.seg[e] + rows - 1) / rows : 0;
+      int scan = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += v;
+      }
+      if (lane == 31) tab.warp_total[warp] = scan;
+      __syncthreads();
+      int prior = lane < THREADS / 32 ? tab.warp_total[lane] : 0;
+      const int sum = warp_sum_int(prior);
+      prior = below + warp_sum_int(lane < warp ? prior : 0);
+      below += sum;
+      if (e < p.experts) tab.tile_start[e] = prior + scan - n;
+      __syncthreads();
+    }
+    tiles_m = below;
+  }
+  const int items = tiles_m * p.tiles_n, mine = worker + (int)threadIdx.x * workers;
+  if (threadIdx.x < LISTED && mine < items) tab.list[threadIdx.x] = find_tile(mine, p, rows, width, tab);
+  __syncthreads();
+  return items;
+}
 
-template <int BN>
+// Scales of one group of four slabs, as this lane stores them: row l of a copy's 32 holds the words of rows l, l + 32, l + 64, l + 96.
+struct Scales {
+  uint4 a, b[2];
+  __device__ __forceinline__ void fetch(const Problem& p, const Tile& t, int row0, int g, int groups, int nblocks, bool wide) {
+    const int lane = threadIdx.x & 31;
+    uint32_t x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __ldg(p.a_scale + (size_t)min(row0 + j * 32 + lane, p.M - 1) * groups + g);
+    a = make_uint4(x[0], x[1], x[2], x[3]);
+    const uint32_t* ws = p.w_scale + (size_t)t.e * nblocks * groups;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (h == 1 && !wide) break;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __ldg(ws + (size_t)min((t.n0 + h * 128 + j * 32 + lane) >> 7, nblocks - 1) * groups + g);
+      b[h] = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* stage, bool wide) const {
+    unsigned char* at = stage + (threadIdx.x & 31) * 16;
+    *reinterpret_cast<uint4*>(at) = a;
+    *reinterpret_cast<uint4*>(at + 512) = b[0];
+    if (wide) *reinterpret_cast<uint4*>(at + 1024) = b[1];
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+};
+
+// ---- epilogue ----------------------------------------------------------------------------------------------------------
+// A lane has a row of accumulators.  Chunks of 32 rows x 64 columns leave through a swizzled buffer in shared memory and a bulk
+// tensor store, which needs one lane (stores of the lanes' own rows, 32 bytes each, keep the load-store unit busy for 64 clocks per
+// 32 columns).
+//
+// GELU(z) = max(z, 0) - |z| Phi(-|z|) and GELU'(z) = Phi(z) + z phi(z), with Phi(-t) = exp(-t^2 / 2) R(t).  R falls from 1/2 and goes as
+// 1 / t: it is u (c1 + c2 u + .. + c5 u^4) in u = 1 / (1 + 0.37677 t), fitted to erfcx in double precision by relative error, 2.9e-5 over
+// 0 <= t <= 14, beyond which the exponential is zero: a hundredth of the rounding to bf16, and of every value, where a polynomial
+// for Phi itself is off by a fixed amount.
+__device__ __forceinline__ void phi_tail2(float z0, float z1, float& p0, float& p1, float& e0, float& e1) {
+  const float s = 0.84932180028801907f;                   // sqrt(log2(e) / 2): exp(-z^2 / 2) = 2^-(s z)^2
+  float x0, x1, u0, u1;
+  unpack2(mul2(pack2(z0, z1), dup2(s)), x0, x1);
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(-x0 * x0));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(-x1 * x1));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u0) : "f"(fmaf(fabsf(z0), 0.37676923076923075f, 1.0f)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u1) : "f"(fmaf(fabsf(z1), 0.37676923076923075f, 1.0f)));
+  const uint64_t u = pack2(u0, u1);
+  uint64_t r = dup2(-0.09088445f);
+  r = fma2(r, u, dup2(0.19726645f));
+  r = fma2(r, u, dup2(0.0858145f));
+  r = fma2(r, u, dup2(0.15798381f));
+  r = fma2(r, u, dup2(0.14980525f));
+  unpack2(mul2(mul2(r, u), pack2(e0, e1)), p0, p1);
+}
+__device__ __forceinline__ void gelu2(float& z0, float& z1) {
+  float p0, p1, e0, e1;
+  phi_tail2(z0, z1, p0, p1, e0, e1);
+  z0 = fmaf(-fabsf(z0), p0, fmaxf(z0, 0.f));
+  z1 = fmaf(-fabsf(z1), p1, fmaxf(z1, 0.f));
+}
+__device__ __forceinline__ void gelu_grad_mul(float& g0, float& g1, float z0, float z1) {
+  float p0, p1, e0, e1;
+  phi_tail2(z0, z1, p0, p1, e0, e1);
+  g0 *= fmaf(z0 * 0.39894228040143268f, e0, z0 < 0.f ? p0 : 1.f - p0);
+  g1 *= fmaf(z1 * 0.39894228040143268f, e1, z1 < 0.f ? p1 : 1.f - p1);
+}
+
+struct Out {
+  bf16* y;
+  bf16* z;                           // the pre-activation, written (act 1, optional) or read (act 2)
+  const float* bias;                 // [experts][N], optional
+  bool release;                      // the next kernel may be scheduled while this one runs
+};
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
+// A warp's staging buffer and what goes through it: 32 rows x 64 columns (one buffer), or 32 x 32 (two: the output's and the
+// pre-activation's, on its way out or in).  16-byte units are swizzled as the tensor maps say.
+template <int CH>
+struct Exit {
+  unsigned char* st;
+  int N;
+  static constexpr int UNITS = CH / 8;
+  __device__ __forceinline__ static uint32_t slot(int r, int u) { return (uint32_t)(r * CH * 2 + ((CH == 64 ? u ^ (r & 7) : u ^ ((r >> 1) & 3)) << 4)); }
+
+  // 32 columns of this lane's row, from unit u0 of buffer b on.
+  __device__ __forceinline__ void stage(const float* v, int b, int u0) const {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[u * 8 + 2 * j], v[u * 8 + 2 * j + 1]);
+        w[j] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      *reinterpret_cast<uint4*>(st + b * 2048 + slot(threadIdx.x & 31, u0 + u)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  // The staged rows row0 .. row0 + 31 of CH columns from col (cols of them wanted) on their way: buffer 0 to out, and where there is
+  // out1 too, buffer 1 to that.  full: no row or column has to be left out that the tensor maps do not leave out by themselves.
+  __device__ __forceinline__ void send(const CUtensorMap* map, bf16* out, const CUtensorMap* map1, bf16* out1, int row0, int r1, int col, int cols, bool full) const {
+    const int lane = threadIdx.x & 31;
+    if (full) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (elected()) {
+        tma_store_2d(map, smem_u32(st), col, row0);
+        if (out1 != nullptr) tma_store_2d(map1, smem_u32(st + 2048), col, row0);
+        stores_commit();
+      }
+    } else {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int r = i * (32 / UNITS) + lane / UNITS, u = lane % UNITS;
+        if (row0 + r < r1 && u * 8 < cols) {
+          const size_t at = (size_t)(row0 + r) * N + col + u * 8;
+          *reinterpret_cast<uint4*>(out + at) = *reinterpret_cast<const uint4*>(st + slot(r, u));
+          if (out1 != nullptr) *reinterpret_cast<uint4*>(out1 + at) = *reinterpret_cast<const uint4*>(st + 2048 + slot(r, u));
+        }
+      }
+    }
+  }
+  // The last store has read its buffers.
+  __device__ __forceinline__ void free_buffers() const {
+    if (elected()) stores_read();
+    __syncwarp();
+  }
+  // The stored pre-activation of a chunk on its way to the second buffer, and this lane's row of it once it is there.
+  __device__ __forceinline__ void ask(const bf16* z, int row0, int r1, int col, int cols) const {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int r = i * (32 / UNITS) + lane / UNITS, u = lane % UNITS;
+      const bool in = row0 + r < r1 && u * 8 < cols;
+      copy16_async(st + 2048 + slot(r, u), in ? z + (size_t)(row0 + r) * N + col + u * 8 : z, in ? 16 : 0);
+    }
+    copies_commit();
+  }
+  __device__ __forceinline__ void got(uint4* w) const {
+    copies_wait<0>();
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) w[u] = *reinterpret_cast<const uint4*>(st + 2048 + slot(threadIdx.x & 31, u));
+    __syncwarp();
+  }
+};
+
+// 32 columns of this lane's row of accumulators, with the bias.
+__device__ __forceinline__ void load_sums(uint32_t taddr, const float* sbias, bool bias, float* v) {
+  uint32_t r[32];
+  tmem_ld32(taddr, r);
+  tmem_ld_wait();
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+  if (bias) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 b = *reinterpret_cast<const float4*>(sbias + j);
+      v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+    }
+  }
+}
+
+// An epilogue warp's way through the tiles.  Of each it has every EPI_SHARE-th chunk of CH columns from its `first` on, rows row0 .. row0 + 31
+// (those below r1; row0 is t.r0 + row_off), columns n0 .. n0 + width - 1 (those below N).  next(t) gives the tiles; ready(i) waits for tile i's sums, which lie at
+// taddr(i); release(i) says that this warp has read them.  What does not depend on the sums -- the bias, the first chunk of the
+// pre-activation -- is asked for a tile ahead.  clipped: the tensor maps end where the rows do (no other expert's rows follow).
+constexpr int chunk_of(int act) { return act == 0 ? 64 : 32; }
+template <int ACT, int BIAS, typename Next, typename Ready, typename Addr, typename Release>
+__device__ __forceinline__ void epilogue(Next next, Ready ready, Addr taddr, Release release, const Out& o, const CUtensorMap* map_y, const CUtensorMap* map_z,
+                                         const Exit<chunk_of(ACT)>& x, int N, int row_off, int width, int first, float* sbias, bool clipped) {
+  constexpr int CH = chunk_of(ACT), STEP = EPI_SHARE * CH, NB = BIAS / 128;
+  const int lane = threadIdx.x & 31;
+  const bool bias = o.bias != nullptr;
+  Tile t, after;
+  float ahead[NB];
+  auto ask_ahead = [&](const Tile& q) {
+    if (bias) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int c = first * CH + i * 32 % CH + i * 32 / CH * STEP + lane;
+        ahead[i] = c < width && q.n0 + c < N ? __ldg(o.bias + (size_t)q.e * N + q.n0 + c) : 0.f;
+      }
+    }
+  };
+  auto any_of = [&](const Tile& q) { return q.r0 + row_off < q.r1 && first * CH < min(width, N - q.n0); };
+  auto ask_z = [&](const Tile& q) {
+    if (ACT == 2 && any_of(q)) x.ask(o.z, q.r0 + row_off, q.r1, q.n0 + first * CH, min(width, N - q.n0) - first * CH);
+  };
+  bool more = next(t);
+  if (more) {
+    ask_ahead(t);
+    ask_z(t);
+  }
+  for (int local = 0; more; ++local) {
+    if (bias) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) sbias[i * 32 + lane] = ahead[i];
+    }
+    more = next(after);
+    if (more) ask_ahead(after);
+    if (!ready(local)) return;
+    __syncwarp();
+    const uint32_t sums = taddr(local);
+    const int row0 = t.r0 + row_off, r1 = t.r1, n0 = t.n0, end = min(n0 + width, N);
+    if (any_of(t)) {
+      const bool rows_full = clipped || row0 + 32 <= r1;
+#pragma unroll 1
+      for (int i = 0, c = first * CH; n0 + c < end; ++i, c += STEP) {
+        const int col = n0 + c, cols = end - col;                         // cols: what is left of the tile
+        const bool full = rows_full && (c + CH <= width || end == N);     // (a tile's last columns leave by themselves)
+        const bool last = cols <= STEP;
+        float v[32];
+        if constexpr (ACT == 0) {
+          load_sums(sums + c, sbias + i * CH, bias, v);
+          x.free_buffers();
+          x.stage(v, 0, 0);
+          if (cols > 32) {
+            load_sums(sums + c + 32, sbias + i * CH + 32, bias, v);
+            x.stage(v, 0, 4);
+          }
+          if (last) release(local);
+          x.send(map_y, o.y, nullptr, nullptr, row0, r1, col, cols, full);
+        } else if constexpr (ACT == 1) {
+          load_sums(sums + c, sbias + i * CH, bias, v);
+          if (last) release(local);
+          x.free_buffers();
+          if (o.z != nullptr) x.stage(v, 1, 0);
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) gelu2(v[j], v[j + 1]);
+          x.stage(v, 0, 0);
+          x.send(map_y, o.y, map_z, o.z, row0, r1, col, cols, full);
+        } else {
+          uint4 zw[4];
+          x.got(zw);
+          if (!last) x.ask(o.z, row0, r1, col + STEP, cols - STEP);
+          else if (more) ask_z(after);
+          load_sums(sums + c, sbias + i * CH, bias, v);
+          if (last) release(local);
+          const uint32_t w[16] = {zw[0].x, zw[0].y, zw[0].z, zw[0].w, zw[1].x, zw[1].y, zw[1].z, zw[1].w, zw[2].x, zw[2].y, zw[2].z, zw[2].w, zw[3].x, zw[3].y, zw[3].z, zw[3].w};
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) gelu_grad_mul(v[j], v[j + 1], __uint_as_float(w[j / 2] << 16), __uint_as_float(w[j / 2] & 0xffff0000u));
+          x.free_buffers();
+          x.stage(v, 0, 0);
+          x.send(map_y, o.y, nullptr, nullptr, row0, r1, col, cols, full);
+        }
+      }
+    } else {
+      if (more) ask_z(after);
+      release(local);
+    }
+    __syncwarp();                    // (the bias is read before the next tile's replaces it)
+    t = after;
+  }
+  if (elected()) stores_read();      // shared memory stays until the last stores have read it
+}
+
+// ---- one CTA a tile ------------------------------------------------------------------------------------------------------
+constexpr int RING_BYTES = 160 * 1024;
+constexpr int stages_for(int bn) { return RING_BYTES / (A_BYTES + bn * BK) < 8 ? RING_BYTES / (A_BYTES + bn * BK) : 8; }
+constexpr int BIAS_BYTES = 64 * 4;   // bias of a warp's columns of a tile: 192 among three
+constexpr int SMEM_BYTES = RING_BYTES + EPI_WARPS * (STAGING_BYTES + BIAS_BYTES) + SF_STAGES * SF_BYTES + 1024;
+constexpr uint32_t SF_COL = 384;     // four columns of A's scales and eight of W's per turn, 16 apart
+
+template <int BN, int ACT>
 __global__ void __launch_bounds__(THREADS, 1)
 gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w,
-                     bf16* __restrict__ C, Problem p, Epi ep, int* status) {
-  constexpr int W_BYTES = BN * BK, STAGE_BYTES = A_BYTES + W_BYTES, STAGES = stages_for(BN), HALF_CHUNKS = BN / 64;
+                     const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z, Problem p, Out out, int* status) {
+  constexpr int W_BYTES = BN * BK, STAGE_BYTES = A_BYTES + W_BYTES, STAGES = stages_for(BN);
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bar_mem[2 * STAGES + 2 * SF_STAGES + 4];
-  __shared__ int tile_start[MAX_E + 1], seg[MAX_E + 1];
-  __shared__ int warp_total[THREADS / 32];
+  __shared__ __align__(16) Tables tab;
   __shared__ uint32_t tmem_base_slot;
   __shared__ int abort_flag;
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-  const uint32_t staging0 = base + STAGES * STAGE_BYTES, sf0 = staging0 + EPI_WARPS * STAGING_BYTES;
+  const uint32_t staging0 = base + STAGES * STAGE_BYTES, sf0 = staging0 + EPI_WARPS * STAGING_BYTES, bias0 = sf0 + SF_STAGES * SF_BYTES;
+  auto ptr = [&](uint32_t a) { return smem_dyn + (a - smem_u32(smem_dyn)); };
   const uint32_t bars = smem_u32(bar_mem);
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
@@ -125,6 +482,8 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     prefetch_map(&map_a);
     prefetch_map(&map_a32);
     prefetch_map(&map_w);
+    prefetch_map(&map_y);
+    prefetch_map(&map_z);
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(&tmem_base_slot), TMEM_COLS);
@@ -134,56 +493,20 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_slot;
-  if (ep.release) release_dependents();
+  if (out.release) release_dependents();
   await_inputs();
   volatile int* abortp = &abort_flag;
-
-  // first tile of every expert: a scan over their row counts (segments are cut to the rows there are, and one that reaches into a later
-  // one to what is before that, so that no row has two)
-  int tiles_m = (p.M + BM - 1) / BM;
-  if (p.seg_start != nullptr) {
-    for (int i = threadIdx.x; i <= p.experts; i += THREADS) seg[i] = min(max(p.seg_start[i], 0), p.M);
-    __syncthreads();
-    int falls = 0;
-    for (int i = threadIdx.x; i < p.experts; i += THREADS) falls |= seg[i + 1] < seg[i];
-    if (__syncthreads_or(falls)) {
-      if (threadIdx.x == 0)
-        for (int i = p.experts - 1; i >= 0; --i) seg[i] = min(seg[i], seg[i + 1]);
-      __syncthreads();
-    }
-    int below = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += THREADS) {
-      const int e = e0 + threadIdx.x;
-      const int n = e < p.experts ? (seg[e + 1] - seg[e] + BM - 1) / BM : 0;
-      int scan = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, scan, o);
-        if (lane >= o) scan += v;
-      }
-      if (lane == 31) warp_total[warp] = scan;
-      __syncthreads();
-      int prior = below;
-      for (int w = 0; w < THREADS / 32; ++w) {
-        const int v = warp_total[w];
-        if (w < warp) prior += v;
-        below += v;
-      }
-      if (e < p.experts) tile_start[e] = prior + scan - n;
-      __syncthreads();
-    }
-    tiles_m = below;
-  }
-  const int work_items = tiles_m * p.tiles_n;
+  Walk walk(blockIdx.x, gridDim.x, make_tables(p, BM, BN, blockIdx.x, gridDim.x, tab));
+  Tile t;
+  auto next = [&]() { return walk.next(t, p, BM, BN, tab); };
 
   if (warp == 0) {
     // ------------------------------- TMA producer -------------------------------
-    if (lane == 0) {
+    if (elected()) {
       int stage = 0, armed = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int w = blockIdx.x; w < work_items && ok; w += gridDim.x) {
-        const Tile t = decode_tile(w, p, tile_start, seg);
+      while (ok && next()) {
         // a tile of few rows takes those alone, 32 at a time; what the ring holds below them enters rows that nobody reads
         const int boxes = (t.r1 - t.r0 + 31) / 32;
         const uint32_t bytes = (uint32_t)(boxes * 32 * BK + W_BYTES);
@@ -194,7 +517,7 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           if (boxes == 4) tma_load_2d(sa, &map_a, full_bar(stage), kb * BK, t.r0);
           else
             for (int j = 0; j < boxes; ++j) tma_load_2d(sa + j * 32 * BK, &map_a32, full_bar(stage), kb * BK, t.r0 + j * 32);
-          tma_load_2d(sa + A_BYTES, &map_w, full_bar(stage), kb * BK, t.e * p.N + t.nt * BN);
+          tma_load_2d(sa + A_BYTES, &map_w, full_bar(stage), kb * BK, t.e * p.N + t.n0);
           ++armed;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
@@ -206,36 +529,42 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     }
   } else if (warp == 1) {
     // ------------------------------- MMA issuer ---------------------------------
-    if (lane == 0) {
-      constexpr uint32_t idesc0 = make_idesc_scaled(BM, BN), KSTEP = UMMA_K >> 4;
+    if (elected()) {
+      const uint32_t idesc0 = make_idesc_scaled(BM, BN);
+      constexpr uint32_t KSTEP = UMMA_K >> 4;
       const uint64_t desc_a0 = make_desc(base, 16, 1024), desc_w0 = make_desc(base + A_BYTES, 16, 1024), desc_s0 = make_desc_scales(sf0);
       int stage = 0, sf = 0, local = 0;
       uint32_t phase = 0, sphase = 0;
-      bool ok = true;
-      for (int w = blockIdx.x; w < work_items && ok; w += gridDim.x, ++local) {
+      bool ok = true, here = false;           // here: this slab's operands were seen to be there
+      for (; ok && next(); ++local) {
         const int buf = local & 1;
-        if (!mbar_wait(tempty_bar(buf), ((local >> 1) & 1) ^ 1u, abortp)) { ok = false; break; }
+        if (!mbar_wait(tempty_bar(buf), ((local >> 1) & 1) ^ 1u, abortp)) break;
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + buf * BN;
         for (int kb = 0; kb < total_kb; ++kb) {
-          const uint32_t sfa = tmem_base + SF_COL + sf * 16, sfb = sfa + 4;
+          const uint32_t sfa = tmem_base + SF_COL + (sf & 1) * 16, sfb = sfa + 4;
           if ((kb & 3) == 0) {
-            if (!mbar_wait(sfull_bar(sf), sphase, abortp)) { ok = false; break; }
+            // (stage sf - 2's barrier: the last time it was there to be emptied, by this turn's products before)
+            if (!mbar_wait(sempty_bar(sf ^ 2), sf < 2 ? sphase ^ 1u : sphase, abortp) || !mbar_wait(sfull_bar(sf), sphase, abortp)) { ok = false; break; }
             tc_fence_after();
             const uint64_t ds = desc_s0 + (uint64_t)((sf * SF_BYTES) >> 4);
             copy_scales(sfa, ds);
             copy_scales(sfb, ds + (512 >> 4));
             if (BN > 128) copy_scales(sfb + 4, ds + (1024 >> 4));
           }
-          if (!mbar_wait(full_bar(stage), phase, abortp)) { ok = false; break; }
+          if (!here && !mbar_wait(full_bar(stage), phase, abortp)) { ok = false; break; }
           tc_fence_after();
+          const int after = stage + 1 == STAGES ? 0 : stage + 1;
+          const uint32_t phase_after = after == 0 ? phase ^ 1u : phase;
+          here = mbar_test(full_bar(after), phase_after);      // (its answer arrives while this slab's instructions are issued)
           const uint64_t off = (uint64_t)((stage * STAGE_BYTES) >> 4);
           const uint32_t idesc = idesc0 | sf_id(kb & 3);
 #pragma unroll
           for (int k = 0; k < BK / UMMA_K; ++k)
             umma_scaled(d_tmem, desc_a0 + off + (uint64_t)(k * KSTEP), desc_w0 + off + (uint64_t)(k * KSTEP), idesc, sfa, sfb, (kb > 0 || k > 0) ? 1u : 0u);
           umma_commit(empty_bar(stage));
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          stage = after;
+          phase = phase_after;
           if ((kb & 3) == 3 || kb == total_kb - 1) {
             umma_commit(sempty_bar(sf));
             if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
@@ -246,63 +575,52 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     }
   } else if (warp == 2) {
     // ------------------------------- scales --------------------------------------
-    // Row l of a copy's 32 holds the words of rows l, l + 32, l + 64 and l + 96.  A word of the next group is fetched while this
-    // one's stage is waited for.
-    int sf = 0;
-    uint32_t sphase = 0;
+    // (words are fetched two groups ahead, across tiles: a group's come from L2, and there may be one group a tile)
     const int nblocks = (p.N + 127) / 128;
-    bool ok = true;
-    for (int w = blockIdx.x; w < work_items && ok; w += gridDim.x) {
-      const Tile t = decode_tile(w, p, tile_start, seg);
-      const uint32_t* ws = p.w_scale + (size_t)t.e * nblocks * groups;
-      uint4 a, b[2];
-      auto fetch = [&](int g) {
-        uint32_t x[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = __ldg(p.a_scale + (size_t)min(t.r0 + j * 32 + lane, p.M - 1) * groups + g);
-        a = make_uint4(x[0], x[1], x[2], x[3]);
-#pragma unroll
-        for (int h = 0; h < (BN > 128 ? 2 : 1); ++h) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = __ldg(ws + (size_t)min((t.nt * BN + h * 128 + j * 32) >> 7, nblocks - 1) * groups + g);
-          b[h] = make_uint4(x[0], x[1], x[2], x[3]);
-        }
-      };
-      fetch(0);
-      for (int g = 0; g < groups; ++g) {
-        ok = __all_sync(0xffffffffu, mbar_wait(sempty_bar(sf), sphase ^ 1u, abortp));
-        if (!ok) break;
-        unsigned char* at = smem_dyn + (sf0 - smem_u32(smem_dyn)) + sf * SF_BYTES + lane * 16;
-        *reinterpret_cast<uint4*>(at) = a;
-        *reinterpret_cast<uint4*>(at + 512) = b[0];
-        if (BN > 128) *reinterpret_cast<uint4*>(at + 1024) = b[1];
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sfull_bar(sf));
-        if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
-        if (g + 1 < groups) fetch(g + 1);
-      }
+    bool more = next();
+    int g = 0, sf = 0;
+    uint32_t sphase = 0;
+    auto fetch = [&](Scales& s) {
+      if (!more) return false;
+      s.fetch(p, t, t.r0, g, groups, nblocks, BN > 128);
+      if (++g == groups) { g = 0; more = next(); }
+      return true;
+    };
+    auto hand = [&](const Scales& s) {
+      if (!warp_wait(sempty_bar(sf), sphase ^ 1u, abortp)) return false;
+      s.store(ptr(sf0 + sf * SF_BYTES), BN > 128);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sfull_bar(sf));
+      if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
+      return true;
+    };
+    Scales s0, s1;
+    bool h0 = fetch(s0), h1 = fetch(s1);
+    while (h0) {
+      if (!hand(s0)) break;
+      h0 = fetch(s0);
+      if (!h1) break;
+      if (!hand(s1)) break;
+      h1 = fetch(s1);
     }
   } else {
     // ------------------------------- epilogue -----------------------------------
-    const int ew = warp - 3, quarter = warp & 3, chalf = ew >> 2;     // (a warp reads the lanes of tensor memory that its number names)
-    unsigned char* st = smem_dyn + (staging0 - smem_u32(smem_dyn)) + ew * STAGING_BYTES;
-    int local = 0;
-    for (int w = blockIdx.x; w < work_items; w += gridDim.x, ++local) {
-      const Tile t = decode_tile(w, p, tile_start, seg);
-      const int buf = local & 1;
-      auto ready = [&]() {
-        const bool r = __all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (local >> 1) & 1, abortp));
-        tc_fence_after();
-        return r;
-      };
-      if (!epilogue_tile<bf16, false, true>(ready, ep, t.e * p.N, C, t.r1, p.N, t.r0 + quarter * 32, t.nt * BN + chalf * HALF_CHUNKS * 32, HALF_CHUNKS,
-                                            tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + chalf * HALF_CHUNKS * 32), st, lane))
-        break;
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(tempty_bar(buf));
-    }
+    const int ew = warp - 3, quarter = warp & 3, first = ew >> 2;    // (a warp reads the lanes of tensor memory that its number names)
+    float* sbias = reinterpret_cast<float*>(ptr(bias0 + ew * BIAS_BYTES));
+    const Exit<chunk_of(ACT)> way = {ptr(staging0 + ew * STAGING_BYTES), p.N};
+    epilogue<ACT, BIAS_BYTES>([&](Tile& q) { return walk.next(q, p, BM, BN, tab); },
+                              [&](int i) {
+                                const bool r = warp_wait(tfull_bar(i & 1), (i >> 1) & 1, abortp);
+                                tc_fence_after();
+                                return r;
+                              },
+                              [&](int i) { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((i & 1) * BN); },
+                              [&](int i) {
+                                tc_fence_before();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(tempty_bar(i & 1));
+                              },
+                              out, &map_y, &map_z, way, p.N, quarter * 32, BN, first, sbias, p.seg_start == nullptr);
   }
   tc_fence_before();
   __syncthreads();
@@ -313,17 +631,281 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   if (threadIdx.x == 0 && abort_flag && status != nullptr) atomicOr(status, STATUS_TIMEOUT);
 }
 
-template <int BN>
-static int launch(const Ctx& c, const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mw, void* C, const Problem& p, const Epi& ep, long tiles) {
-  auto kern = gemm_block128_kernel<BN>;
+// ---- two CTAs a tile -------------------------------------------------------------------------------------------------------
+// As gemm_tc2.cu: each SM stages its own 128 rows of A and half of the columns of W, 31 KB a slab for 256 x 240 sums where one CTA
+// takes 40 KB for 128 x 192: the L2-to-SM path bounds both (about 50 bytes a clock and SM).  Both CTAs hold the scales of their own rows and of
+// all columns.  `width` columns a tile, a multiple of 16, is chosen for each product: up to 240, so that two accumulators and two turns
+// of scales fit tensor memory.
+constexpr int P_WIDTH = 240, P_STAGES = 5, P_BIAS_BYTES = 128 * 4;
+constexpr int P_STAGE_BYTES = A_BYTES + P_WIDTH / 2 * BK;
+constexpr int P_SMEM_BYTES = P_STAGES * P_STAGE_BYTES + EPI_WARPS * (STAGING_BYTES + P_BIAS_BYTES) + SF_STAGES * SF_BYTES + 1024;
+constexpr uint32_t P_SF_COL = 2 * P_WIDTH;
+static_assert(P_SF_COL + 16 + 12 <= TMEM_COLS && P_STAGE_BYTES % 1024 == 0, "the scales fit behind the accumulators");
+
+__device__ __forceinline__ void umma_scaled_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void copy_scales_pair(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+template <int ACT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w,
+                          const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z, Problem p, Out out, int width, int* status) {
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ __align__(8) unsigned long long bar_mem[2 * P_STAGES + 2 * SF_STAGES + 4];
+  __shared__ __align__(16) Tables tab;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int abort_flag;
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  const uint32_t staging0 = base + P_STAGES * P_STAGE_BYTES, sf0 = staging0 + EPI_WARPS * STAGING_BYTES, bias0 = sf0 + SF_STAGES * SF_BYTES;
+  auto ptr = [&](uint32_t a) { return smem_dyn + (a - smem_u32(smem_dyn)); };
+  const uint32_t bars = smem_u32(bar_mem);
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (P_STAGES + s); };
+  auto sfull_bar = [&](int s) { return bars + 8u * (2 * P_STAGES + s); };
+  auto sempty_bar = [&](int s) { return bars + 8u * (2 * P_STAGES + SF_STAGES + s); };
+  auto tfull_bar = [&](int b) { return bars + 8u * (2 * P_STAGES + 2 * SF_STAGES + b); };
+  auto tempty_bar = [&](int b) { return bars + 8u * (2 * P_STAGES + 2 * SF_STAGES + 2 + b); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int total_kb = (p.K + BK - 1) / BK, groups = (total_kb + 3) / 4;
+  const int rank = (int)cluster_rank();
+  const bool leader = rank == 0;
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < P_STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < SF_STAGES; ++s) { mbar_init(sfull_bar(s), 2); mbar_init(sempty_bar(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * EPI_WARPS); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_a);
+    prefetch_map(&map_a32);
+    prefetch_map(&map_w);
+    prefetch_map(&map_y);
+    prefetch_map(&map_z);
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_base_slot), TMEM_COLS);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync_all();                       // barriers of both CTAs exist before anyone signals them
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_slot;
+  await_inputs();                           // (fills the SMs: see release_dependents)
+  volatile int* abortp = &abort_flag;
+  Walk walk(blockIdx.x >> 1, gridDim.x >> 1, make_tables(p, 2 * BM, width, blockIdx.x >> 1, gridDim.x >> 1, tab));
+  Tile t;
+  auto next = [&]() { return walk.next(t, p, 2 * BM, width, tab); };
+  auto rows_of = [&](int r) { return min(max(t.r1 - t.r0 - r * BM, 0), BM); };
+
+  if (warp == 0) {
+    // ------------------------------- TMA producer (both CTAs) -------------------------------
+    if (elected()) {
+      int stage = 0, armed = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const int cols = width >> 1;
+      while (ok && next()) {
+        const int boxes = (rows_of(rank) + 31) / 32, row0 = t.r0 + rank * BM;
+        const uint32_t bytes = (uint32_t)(((rows_of(0) + 31) / 32 + (rows_of(1) + 31) / 32) * 32 * BK + width * BK);
+        for (int kb = 0; kb < total_kb; ++kb) {
+          if (!mbar_wait(empty_bar(stage), phase ^ 1u, abortp)) { ok = false; break; }
+          const uint32_t fb = full_bar(stage) & PEER_MASK;      // the leader's barrier collects both CTAs' bytes
+          if (leader) mbar_expect_tx(full_bar(stage), bytes);
+          const uint32_t sa = base + stage * P_STAGE_BYTES;
+          if (boxes == 4) tma_load_2d_pair(sa, &map_a, fb, kb * BK, row0);
+          else
+            for (int j = 0; j < boxes; ++j) tma_load_2d_pair(sa + j * 32 * BK, &map_a32, fb, kb * BK, row0 + j * 32);
+          tma_load_2d_pair(sa + A_BYTES, &map_w, fb, kb * BK, t.e * p.N + t.n0 + rank * cols);
+          ++armed;
+          if (++stage == P_STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok && armed > 0) {
+        unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 1000000ull) {}
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------- MMA issuer (leader CTA only) ---------------------------
+    if (leader && elected()) {
+      const uint32_t idesc0 = make_idesc_scaled(2 * BM, width);
+      constexpr uint32_t KSTEP = UMMA_K >> 4;
+      const uint64_t desc_a0 = make_desc(base, 16, 1024), desc_w0 = make_desc(base + A_BYTES, 16, 1024), desc_s0 = make_desc_scales(sf0);
+      int stage = 0, sf = 0, local = 0;
+      uint32_t phase = 0, sphase = 0;
+      bool ok = true, here = false;           // here: this slab's operands were seen to be there
+      for (; ok && next(); ++local) {
+        const int buf = local & 1;
+        if (!mbar_wait(tempty_bar(buf), ((local >> 1) & 1) ^ 1u, abortp)) break;
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + buf * P_WIDTH;
+        for (int kb = 0; kb < total_kb; ++kb) {
+          const uint32_t sfa = tmem_base + P_SF_COL + (sf & 1) * 16, sfb = sfa + 4;
+          if ((kb & 3) == 0) {
+          // (the other CTA's scales were written by its own threads: the wait takes part in the cluster's order)
+            if (!mbar_wait(sempty_bar(sf ^ 2), sf < 2 ? sphase ^ 1u : sphase, abortp) || !mbar_wait(sfull_bar(sf), sphase, abortp) || !mbar_try_wait_cluster(sfull_bar(sf), sphase)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint64_t ds = desc_s0 + (uint64_t)((sf * SF_BYTES) >> 4);
+            copy_scales_pair(sfa, ds);
+            copy_scales_pair(sfb, ds + (512 >> 4));
+            if (width > 128) copy_scales_pair(sfb + 4, ds + (1024 >> 4));
+          }
+          if (!here && !mbar_wait(full_bar(stage), phase, abortp)) { ok = false; break; }
+          tc_fence_after();
+          const int after = stage + 1 == P_STAGES ? 0 : stage + 1;
+          const uint32_t phase_after = after == 0 ? phase ^ 1u : phase;
+          here = mbar_test(full_bar(after), phase_after);      // (its answer arrives while this slab's instructions are issued)
+          const uint64_t off = (uint64_t)((stage * P_STAGE_BYTES) >> 4);
+          const uint32_t idesc = idesc0 | sf_id(kb & 3);
+#pragma unroll
+          for (int k = 0; k < BK / UMMA_K; ++k)
+            umma_scaled_pair(d_tmem, desc_a0 + off + (uint64_t)(k * KSTEP), desc_w0 + off + (uint64_t)(k * KSTEP), idesc, sfa, sfb, (kb > 0 || k > 0) ? 1u : 0u);
+          umma_commit_pair(empty_bar(stage));
+          stage = after;
+          phase = phase_after;
+          if ((kb & 3) == 3 || kb == total_kb - 1) {
+            umma_commit_pair(sempty_bar(sf));
+            if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
+          }
+        }
+        if (ok) umma_commit_pair(tfull_bar(buf));
+      }
+    }
+  } else if (warp == 2) {
+    // ------------------------------- scales (both CTAs) --------------------------------------
+    // (words are fetched two groups ahead, across tiles: a group's come from L2, and there may be one group a tile)
+    const int nblocks = (p.N + 127) / 128;
+    bool more = next();
+    int g = 0, sf = 0;
+    uint32_t sphase = 0;
+    auto fetch = [&](Scales& s) {
+      if (!more) return false;
+      s.fetch(p, t, t.r0 + rank * BM, g, groups, nblocks, width > 128);
+      if (++g == groups) { g = 0; more = next(); }
+      return true;
+    };
+    auto hand = [&](const Scales& s) {
+      if (!warp_wait(sempty_bar(sf), sphase ^ 1u, abortp)) return false;
+      s.store(ptr(sf0 + sf * SF_BYTES), width > 128);
+      __syncwarp();
+      if (lane == 0) mbar_arrive_leader(sfull_bar(sf));
+      if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
+      return true;
+    };
+    Scales s0, s1;
+    bool h0 = fetch(s0), h1 = fetch(s1);
+    while (h0) {
+      if (!hand(s0)) break;
+      h0 = fetch(s0);
+      if (!h1) break;
+      if (!hand(s1)) break;
+      h1 = fetch(s1);
+    }
+  } else {
+    // ------------------------------- epilogue (both CTAs, own rows) --------------------------
+    const int ew = warp - 3, quarter = warp & 3, first = ew >> 2;
+    float* sbias = reinterpret_cast<float*>(ptr(bias0 + ew * P_BIAS_BYTES));
+    const Exit<chunk_of(ACT)> way = {ptr(staging0 + ew * STAGING_BYTES), p.N};
+    epilogue<ACT, P_BIAS_BYTES>([&](Tile& q) { return walk.next(q, p, 2 * BM, width, tab); },
+                                [&](int i) {
+                                  const bool r = warp_wait(tfull_bar(i & 1), (i >> 1) & 1, abortp);
+                                  tc_fence_after();
+                                  return r;
+                                },
+                                [&](int i) { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((i & 1) * P_WIDTH); },
+                                [&](int i) {
+                                  tc_fence_before();
+                                  __syncwarp();
+                                  if (lane == 0) mbar_arrive_leader_relaxed(tempty_bar(i & 1));
+                                },
+                                out, &map_y, &map_z, way, p.N, rank * BM + quarter * 32, width, first, sbias, p.seg_start == nullptr);
+  }
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();                       // neither CTA leaves while the other may still touch its memory
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, TMEM_COLS);
+  }
+  if (threadIdx.x == 0 && abort_flag && status != nullptr) atomicOr(status, STATUS_TIMEOUT);
+}
+
+template <int BN, int ACT>
+static int launch(const Ctx& c, const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mw, const CUtensorMap& my, const CUtensorMap& mz, const Problem& p, const Out& o, long tiles) {
+  auto kern = gemm_block128_kernel<BN, ACT>;
   static SmemLimit lim;
   if (!ensure_smem(lim, kern, SMEM_BYTES)) return -3;
   const int sms = c.sm_count > 0 ? c.sm_count : B200_SMS, grid = (int)(tiles < sms ? tiles : sms);
-  Epi epi = ep;
-  epi.release = 2 * grid <= sms;
+  Out out = o;
+  out.release = 2 * grid <= sms;
   note_launch(1);
-  launch_k(kern, grid, THREADS, SMEM_BYTES, c.stream, ma, ma32, mw, (bf16*)C, p, epi, c.status);
+  launch_k(kern, grid, THREADS, SMEM_BYTES, c.stream, ma, ma32, mw, my, mz, p, out, c.status);
   return 0;
+}
+template <int ACT>
+static int launch_pair(const Ctx& c, const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mw, const CUtensorMap& my, const CUtensorMap& mz, const Problem& p, const Out& o, int width, long tiles) {
+  auto kern = gemm_block128_pair_kernel<ACT>;
+  static SmemLimit lim;
+  if (!ensure_smem(lim, kern, P_SMEM_BYTES)) return -3;
+  const int pairs = (c.sm_count > 0 ? c.sm_count : B200_SMS) / 2;
+  note_launch(1);
+  launch_k(kern, 2 * (int)(tiles < pairs ? tiles : pairs), THREADS, P_SMEM_BYTES, c.stream, ma, ma32, mw, my, mz, p, o, width, c.status);
+  return 0;
+}
+
+// Rows of bf16 outputs in boxes of 32 rows x `cols` columns (64 or 32), swizzled over a row of the box.
+static bool make_out_map(CUtensorMap* map, const void* ptr, int n, int m, int cols) {
+  EncodeFn fn = encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m};
+  cuuint64_t strides[1] = {(cuuint64_t)n * 2};
+  cuuint32_t box[2] = {(cuuint32_t)cols, 32};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Width of a pair's tiles: the number of waves times what a slab of such a tile takes (its bytes at 50 a clock and SM).
+static int pair_width(long tiles_m, int n, int pairs) {
+  int best = P_WIDTH;
+  double t_best = 1e30;
+  for (int w = P_WIDTH; w >= 128; w -= 16) {
+    const double t = (double)((tiles_m * ceil_div(n, w) + pairs - 1) / pairs) * (BM + w / 2 + 24);
+    if (t < t_best) { t_best = t; best = w; }
+  }
+  return best;
+}
+
+// us of a launch in a row of launches, one CTA a tile and two:
+//   25216 x 2304 x 384    34.5 / 37.0      25216 x 2304 x 768    54.9 / 51.5      25216 x 2304 x 1536   88 / 82       6304 x 2304 x 768    17.7 / 18.7
+//   25216 x 384 x 1536    18.1 / 20.2      4096 x 4096 x 4096    59.2 / 53.2      8192 x 4096 x 7168    203 / 179
+// Two take fewer bytes a slab but longer to fill and drain, so they want a long k, several waves and columns for wide tiles; and rows: an
+// expert's last tile is half empty on average.
+static bool use_pairs(int m, int n, int k, int experts, int sms) {
+  const long tiles = (long)ceil_div(m, 2 * BM) * ceil_div(n, P_WIDTH);
+  return k >= 768 && n >= 768 && m / experts >= 512 && tiles * k >= 2l * sms * 1024;
 }
 
 }  // namespace tcb
@@ -333,19 +915,31 @@ int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void*
                   const GemmEpilogue& e) {
   using namespace tcb;
   const int sms = c.sm_count > 0 ? c.sm_count : B200_SMS;
-  const long tiles_m = seg_start != nullptr ? ceil_div(m, BM) + (long)(experts < m ? experts : m) - 1 : ceil_div(m, BM);      // at most
-  const int bn = tiles_m * ceil_div(n, 64) <= sms ? 64 : tiles_m * ceil_div(n, 128) <= sms ? 128 : 192;
-  CUtensorMap ma, ma32, mw;
+  const long some = seg_start != nullptr ? (experts < m ? experts : m) - 1 : 0;      // at most so many tiles more than the rows alone would take
+  const long tiles_m = ceil_div(m, BM) + some;
+  const bool pair = use_pairs(m, n, k, experts, sms);
+  const int bn = pair ? pair_width(ceil_div(m, 2 * BM) + some / 2, n, sms / 2) : tiles_m * ceil_div(n, 64) <= sms ? 64 : tiles_m * ceil_div(n, 128) <= sms ? 128 : 192;
+  bf16* z = (bf16*)(e.act == 1 ? e.aux_out : const_cast<void*>(e.aux_in));
+  CUtensorMap ma, ma32, mw, my, mz;
+  if (!make_out_map(&my, C, n, m, chunk_of(e.act)) || !make_out_map(&mz, z != nullptr ? z : C, n, m, chunk_of(e.act))) return -2;
   if (!make_map_u8(&ma, Aq, (uint64_t)k, (uint64_t)m, (uint64_t)k, BM) || !make_map_u8(&ma32, Aq, (uint64_t)k, (uint64_t)m, (uint64_t)k, 32) ||
-      !make_map_u8(&mw, Wq, (uint64_t)k, (uint64_t)experts * n, (uint64_t)k, bn))
+      !make_map_u8(&mw, Wq, (uint64_t)k, (uint64_t)experts * n, (uint64_t)k, pair ? bn / 2 : bn))
     return -2;
   Problem p;
   p.M = m; p.N = n; p.K = k; p.tiles_n = ceil_div(n, bn); p.experts = experts; p.seg_start = seg_start;
   p.a_scale = (const uint32_t*)a_scale; p.w_scale = (const uint32_t*)w_scale;
-  Epi ep;
-  ep.bias = e.bias; ep.act = e.act; ep.aux_out = e.aux_out; ep.aux_in = e.aux_in;
-  const long tiles = tiles_m * p.tiles_n;
-  return bn == 64 ? launch<64>(c, ma, ma32, mw, C, p, ep, tiles) : bn == 128 ? launch<128>(c, ma, ma32, mw, C, p, ep, tiles) : launch<192>(c, ma, ma32, mw, C, p, ep, tiles);
+  Out o;
+  o.y = (bf16*)C;
+  o.z = z;
+  o.bias = e.bias;
+  o.release = false;
+  const long tiles = (pair ? ceil_div(m, 2 * BM) + some : tiles_m) * p.tiles_n;
+  auto go = [&](auto act) {
+    constexpr int A = decltype(act)::value;
+    if (pair) return launch_pair<A>(c, ma, ma32, mw, my, mz, p, o, bn, tiles);
+    return bn == 64 ? launch<64, A>(c, ma, ma32, mw, my, mz, p, o, tiles) : bn == 128 ? launch<128, A>(c, ma, ma32, mw, my, mz, p, o, tiles) : launch<192, A>(c, ma, ma32, mw, my, mz, p, o, tiles);
+  };
+  return e.act == 0 ? go(std::integral_constant<int, 0>()) : e.act == 1 ? go(std::integral_constant<int, 1>()) : go(std::integral_constant<int, 2>());
 }
 
 }  // namespace bsr

@@ -187,16 +187,16 @@ def near(got, want, mag, k, lip=1.0, off=0.0):
 
 
 def phi_off(z):
-    """The kernel forms Phi within 7e-6 of its value for |z| <= 5.75: Phi(-t) = exp(-t^2 / 2) R(t).  Beyond it takes R(5.75) for R(t).
-    R(t) sqrt(2 pi) is Mills' ratio, which falls, and t R(t) rises: R(5.75) / R(t) < t / 5.75, so that Phi is too large there by less
-    than (t / 5.75 - 1) Phi(-t), 5e-9 at most.  An exponential below 2^-126 is flushed to zero."""
-    return 2.0 ** -126 + 7e-6 * P.phi(z) + np.maximum(np.abs(z) / 5.75 - 1.0, 0.0) * P.phi(-np.abs(z))
+    """The kernel forms Phi(-t) = exp(-t^2 / 2) R(t) with an R that is within 2.9e-5 of its value for every t; the exponential is 2 to a
+    power of up to 126 that is rounded to 2^-24 of itself, twice: 126 * 2^-23 * ln 2 = 1.04e-5; and nine operations of at most 2^-22 each.
+    An exponential below 2^-126 is flushed to zero."""
+    return 2.0 ** -126 + (2.9e-5 + 1.04e-5 + 9 * 2.0 ** -22) * P.phi(z)
 
 
 def gelu_grad_off(z):
-    """GELU' = Phi + z phi, two terms of either sign: near z = -0.75 they cancel, and what each is off by (z phi: the exponential's
-    and the products' roundings, below 7e-6 too) is not small beside their sum."""
-    return phi_off(z) + 2.0 ** -126 * np.abs(z) + 7e-6 * np.abs(z) * np.exp(-0.5 * z * z) / np.sqrt(2.0 * np.pi)
+    """GELU' = Phi + z phi, two terms of either sign: near z = -0.75 they cancel, and what each is off by is not small beside
+    their sum.  z phi has the exponential's error and some products' roundings; above zero Phi is 1 - Phi(-z)."""
+    return phi_off(-np.abs(z)) + 2.0 ** -22 * P.phi(z) + (2.0 ** -126 + (1.04e-5 + 9 * 2.0 ** -22) * np.exp(-0.5 * z * z) / np.sqrt(2.0 * np.pi)) * np.abs(z)
 
 
 def check(got, zgot, act, part, mag, z, k):
@@ -204,7 +204,7 @@ def check(got, zgot, act, part, mag, z, k):
         near(got, part, mag, k)
     elif act == 1:
         near(zgot, part, mag, k)
-        near(got, P.gelu(part), mag, k, 1.13, np.abs(part) * phi_off(part))            # |GELU'| < 1.13
+        near(got, P.gelu(part), mag, k, 1.13, np.abs(part) * phi_off(-np.abs(part)))     # |GELU'| < 1.13; the tail is what is approximated
     else:
         near(got, part * P.gelu_grad(z), mag * np.abs(P.gelu_grad(z)), k, 1.0, np.abs(part) * gelu_grad_off(z))
 

@@ -852,6 +852,218 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
   if (threadIdx.x == 0 && abort_flag && status != nullptr) atomicOr(status, STATUS_TIMEOUT);
 }
 
+// ---- few tiles: a tile's k over a cluster -----------------------------------------------------------------------------------
+// What bounds a product of few rows is latency: 16 x 4096 x 4096 is 64 tiles with 32 slabs one after the other.  As in gemm_tc_small.cu
+// a tile's k is split over the CTAs of a cluster (in groups of four slabs, whole words of scales), which send each other their partial sums through
+// distributed shared memory; each adds up and finishes an equal share of the rows, in the order of k.
+constexpr int S_BN = 64, S_STAGES = 6, S_MAX_SPLITS = 8, S_THREADS = 256;
+constexpr int S_STAGE_BYTES = A_BYTES + S_BN * BK;
+constexpr int S_RECV_BYTES = (BM + S_MAX_SPLITS) * S_BN * 4;          // shares of the rows are rounded up
+constexpr int S_SMEM_BYTES = S_STAGES * S_STAGE_BYTES + S_RECV_BYTES + SF_STAGES * SF_BYTES + 1024;
+constexpr uint32_t S_TMEM_COLS = 128, S_SF_COL = S_BN;
+constexpr int S_PASSES = BM / 2 / 16;                                  // a CTA finishes 16 rows a pass
+
+template <int ACT>
+__global__ void __launch_bounds__(S_THREADS)
+gemm_block128_small_kernel(const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w, Problem p, Out out, int* status) {
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ __align__(8) unsigned long long bar_mem[2 * S_STAGES + 2 * SF_STAGES + 1];
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int abort_flag;
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  const uint32_t recv = base + S_STAGES * S_STAGE_BYTES, sf0 = recv + S_RECV_BYTES;
+  auto ptr = [&](uint32_t a) { return smem_dyn + (a - smem_u32(smem_dyn)); };
+  const uint32_t bars = smem_u32(bar_mem);
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (S_STAGES + s); };
+  auto sfull_bar = [&](int s) { return bars + 8u * (2 * S_STAGES + s); };
+  auto sempty_bar = [&](int s) { return bars + 8u * (2 * S_STAGES + SF_STAGES + s); };
+  const uint32_t done_bar = bars + 8u * (2 * S_STAGES + 2 * SF_STAGES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.z, splits = gridDim.z;
+  const int total_kb = (p.K + BK - 1) / BK, groups = (total_kb + 3) / 4;
+  const int g0 = rank * groups / splits, g1 = (rank + 1) * groups / splits, kb0 = g0 * 4, nkb = min(g1 * 4, total_kb) - kb0;
+  Tile t;
+  t.e = 0;
+  t.r0 = blockIdx.y * BM;
+  t.r1 = min(p.M, t.r0 + BM);
+  t.n0 = blockIdx.x * S_BN;
+  // an equal share of the tile's rows for every CTA of the cluster; this one's are q0 to q1 - 1
+  const int rows = t.r1 - t.r0, share = (rows + splits - 1) / splits, q0 = min(rank * share, rows), q1 = min(rows, q0 + share);
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < S_STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < SF_STAGES; ++s) { mbar_init(sfull_bar(s), 1); mbar_init(sempty_bar(s), 1); }
+    mbar_init(done_bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_a32);
+    prefetch_map(&map_w);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&tmem_base_slot), S_TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  cluster_arrive();                        // this CTA has started: the others may write to its shared memory
+  const uint32_t tmem_base = tmem_base_slot;
+  release_dependents();
+  await_inputs();
+  volatile int* abortp = &abort_flag;
+
+  if (warp == 0) {
+    if (elected()) {
+      const int boxes = (rows + 31) / 32;
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int i = 0; i < nkb; ++i) {
+        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abortp)) break;
+        mbar_expect_tx(full_bar(stage), (uint32_t)(boxes * 32 * BK + S_BN * BK));
+        const uint32_t sa = base + stage * S_STAGE_BYTES;
+        tma_load_2d(sa + A_BYTES, &map_w, full_bar(stage), (kb0 + i) * BK, t.n0);
+        for (int j = 0; j < boxes; ++j) tma_load_2d(sa + j * 32 * BK, &map_a32, full_bar(stage), (kb0 + i) * BK, t.r0 + j * 32);
+        if (++stage == S_STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    if (elected()) {
+      constexpr uint32_t idesc0 = make_idesc_scaled(BM, S_BN), KSTEP = UMMA_K >> 4;
+      const uint64_t desc_a0 = make_desc(base, 16, 1024), desc_w0 = make_desc(base + A_BYTES, 16, 1024), desc_s0 = make_desc_scales(sf0);
+      int stage = 0, sf = 0;
+      uint32_t phase = 0, sphase = 0;
+      for (int i = 0; i < nkb; ++i) {
+        const uint32_t sfa = tmem_base + S_SF_COL + sf * 8, sfb = sfa + 4;           // (four columns each; as many turns as stages)
+        if ((i & 3) == 0) {
+          if (!mbar_wait(sfull_bar(sf), sphase, abortp)) break;
+          tc_fence_after();
+          const uint64_t ds = desc_s0 + (uint64_t)((sf * SF_BYTES) >> 4);
+          copy_scales(sfa, ds);
+          copy_scales(sfb, ds + (512 >> 4));
+        }
+        if (!mbar_wait(full_bar(stage), phase, abortp)) break;
+        tc_fence_after();
+        const uint64_t off = (uint64_t)((stage * S_STAGE_BYTES) >> 4);
+        const uint32_t idesc = idesc0 | sf_id(i & 3);
+#pragma unroll
+        for (int k = 0; k < BK / UMMA_K; ++k)
+          umma_scaled(tmem_base, desc_a0 + off + (uint64_t)(k * KSTEP), desc_w0 + off + (uint64_t)(k * KSTEP), idesc, sfa, sfb, (i > 0 || k > 0) ? 1u : 0u);
+        umma_commit(empty_bar(stage));
+        if (++stage == S_STAGES) { stage = 0; phase ^= 1u; }
+        if ((i & 3) == 3) {
+          umma_commit(sempty_bar(sf));
+          if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
+        }
+      }
+      umma_commit(done_bar);               // after a wait that gave up: of what was issued
+    }
+  } else if (warp == 2) {
+    const int nblocks = (p.N + 127) / 128;
+    int sf = 0;
+    uint32_t sphase = 0;
+    Scales s;
+    s.fetch(p, t, t.r0, g0, groups, nblocks, false);
+    for (int g = g0; g < g1; ++g) {
+      if (!warp_wait(sempty_bar(sf), sphase ^ 1u, abortp)) break;
+      s.store(ptr(sf0 + sf * SF_BYTES), false);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sfull_bar(sf));
+      if (++sf == SF_STAGES) { sf = 0; sphase ^= 1u; }
+      if (g + 1 < g1) s.fetch(p, t, t.r0, g + 1, groups, nblocks, false);
+    }
+  }
+  __syncwarp();
+
+  // what the epilogue of this CTA's rows reads, 16 rows a pass: a thread has four columns of a row
+  const int unit = threadIdx.x & 15, sub = threadIdx.x >> 4, col = t.n0 + unit * 4;
+  auto at = [&](int r) { return (size_t)(t.r0 + r) * p.N + col; };
+  auto mine = [&](int i) { return q0 + i * 16 + sub < q1 && col < p.N; };
+  float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
+  float z[S_PASSES][4];
+  if (out.bias != nullptr && col < p.N) bias = __ldg(reinterpret_cast<const float4*>(out.bias + col));
+  if constexpr (ACT == 2) {
+#pragma unroll
+    for (int i = 0; i < S_PASSES; ++i)
+      if (mine(i)) load4(out.z + at(q0 + i * 16 + sub), z[i]);
+  }
+
+  // accumulators -> their rows' owners: [splits][share][64], a row's 16-byte units permuted by the row (no bank conflicts)
+  const bool ok = warp_wait(done_bar, 0, abortp);
+  tc_fence_after();
+  cluster_wait();
+  if (ok) {
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    uint32_t r[32];
+    tmem_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 32), r);
+    tmem_ld_wait();
+    if (row < rows) {
+      const int owner = row / share, local = row - owner * share;
+      const uint32_t dst = peer_addr(recv + (uint32_t)(rank * share + local) * (S_BN * 4), owner);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) send16(dst + (((half * 8 + u) ^ (local & 7)) << 4), r + 4 * u);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, S_TMEM_COLS);
+  }
+
+  const float* got = reinterpret_cast<const float*>(ptr(recv));
+#pragma unroll
+  for (int i = 0; i < S_PASSES; ++i) {
+    if (!mine(i) || !ok) continue;
+    const int local = i * 16 + sub;
+    const float* src = got + local * S_BN + ((unit ^ (local & 7)) << 2);
+    float v[4] = {bias.x, bias.y, bias.z, bias.w};
+    float4 x[S_MAX_SPLITS];
+#pragma unroll
+    for (int q = 0; q < S_MAX_SPLITS; ++q)
+      if (q < splits) x[q] = *reinterpret_cast<const float4*>(src + q * share * S_BN);
+    float4 sum = x[0];
+#pragma unroll
+    for (int q = 1; q < S_MAX_SPLITS; ++q)
+      if (q < splits) { sum.x += x[q].x; sum.y += x[q].y; sum.z += x[q].z; sum.w += x[q].w; }
+    v[0] += sum.x; v[1] += sum.y; v[2] += sum.z; v[3] += sum.w;
+    if constexpr (ACT == 1) {
+      if (out.z != nullptr) store4(out.z + at(q0 + local), v);
+      gelu2(v[0], v[1]);
+      gelu2(v[2], v[3]);
+    } else if constexpr (ACT == 2) {
+      gelu_grad_mul(v[0], v[1], z[i][0], z[i][1]);
+      gelu_grad_mul(v[2], v[3], z[i][2], z[i][3]);
+    }
+    store4(out.y + at(q0 + local), v);
+  }
+  if (threadIdx.x == 0 && abort_flag) {
+    unsigned long long t0 = global_ns();   // copies already issued still land in shared memory
+    while (global_ns() - t0 < 1000000ull) {}
+    if (status != nullptr) atomicOr(status, STATUS_TIMEOUT);
+  }
+}
+
+// Splits of a tile's k range, 0: not a product for this kernel.  As many as still fit the SMs in one wave, each with a group of slabs at least.
+static int small_splits(int m, int n, int k, int sms) {
+  const long tiles = (long)ceil_div(m, BM) * ceil_div(n, S_BN);
+  const int groups = ceil_div(k, 4 * BK);
+  int s = 1;
+  while (s < S_MAX_SPLITS && tiles * s * 2 <= sms && groups >= s * 2) s *= 2;
+  return s >= 2 ? s : 0;
+}
+template <int ACT>
+static int launch_small(const Ctx& c, const CUtensorMap& ma32, const CUtensorMap& mw, const Problem& p, const Out& o, int splits) {
+  auto kern = gemm_block128_small_kernel<ACT>;
+  static SmemLimit lim;
+  if (!ensure_smem(lim, kern, S_SMEM_BYTES)) return -3;
+  note_launch(1);
+  launch_cluster(kern, dim3(ceil_div(p.N, S_BN), ceil_div(p.M, BM), splits), S_THREADS, S_SMEM_BYTES, c.stream, dim3(1, 1, splits), ma32, mw, p, o, c.status);
+  return 0;
+}
+
 template <int BN, int ACT>
 static int launch(const Ctx& c, const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mw, const CUtensorMap& my, const CUtensorMap& mz, const Problem& p, const Out& o, long tiles) {
   auto kern = gemm_block128_kernel<BN, ACT>;
@@ -917,8 +1129,9 @@ int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void*
   const int sms = c.sm_count > 0 ? c.sm_count : B200_SMS;
   const long some = seg_start != nullptr ? (experts < m ? experts : m) - 1 : 0;      // at most so many tiles more than the rows alone would take
   const long tiles_m = ceil_div(m, BM) + some;
-  const bool pair = use_pairs(m, n, k, experts, sms);
-  const int bn = pair ? pair_width(ceil_div(m, 2 * BM) + some / 2, n, sms / 2) : tiles_m * ceil_div(n, 64) <= sms ? 64 : tiles_m * ceil_div(n, 128) <= sms ? 128 : 192;
+  const int splits = seg_start == nullptr ? small_splits(m, n, k, sms) : 0;
+  const bool pair = splits == 0 && use_pairs(m, n, k, experts, sms);
+  const int bn = splits > 0 ? S_BN : pair ? pair_width(ceil_div(m, 2 * BM) + some / 2, n, sms / 2) : tiles_m * ceil_div(n, 64) <= sms ? 64 : tiles_m * ceil_div(n, 128) <= sms ? 128 : 192;
   bf16* z = (bf16*)(e.act == 1 ? e.aux_out : const_cast<void*>(e.aux_in));
   CUtensorMap ma, ma32, mw, my, mz;
   if (!make_out_map(&my, C, n, m, chunk_of(e.act)) || !make_out_map(&mz, z != nullptr ? z : C, n, m, chunk_of(e.act))) return -2;
@@ -936,6 +1149,7 @@ int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void*
   const long tiles = (pair ? ceil_div(m, 2 * BM) + some : tiles_m) * p.tiles_n;
   auto go = [&](auto act) {
     constexpr int A = decltype(act)::value;
+    if (splits > 0) return launch_small<A>(c, ma32, mw, p, o, splits);
     if (pair) return launch_pair<A>(c, ma, ma32, mw, my, mz, p, o, bn, tiles);
     return bn == 64 ? launch<64, A>(c, ma, ma32, mw, my, mz, p, o, tiles) : bn == 128 ? launch<128, A>(c, ma, ma32, mw, my, mz, p, o, tiles) : launch<192, A>(c, ma, ma32, mw, my, mz, p, o, tiles);
   };

@@ -212,6 +212,8 @@ def check(got, zgot, act, part, mag, z, k):
 @gpu
 @pytest.mark.parametrize("act", [0, 1, 2])
 @pytest.mark.parametrize("m,n,k", [(1, 8, 16), (1, 264, 144), (33, 72, 512), (127, 64, 128), (128, 128, 640), (129, 200, 528), (300, 1000, 1040), (64, 384, 1536), (97, 2304, 768),
+                                   # few tiles: k over 2, 4 and 8 CTAs, shares of rows that do not come out even
+                                   (1, 2000, 7168), (7, 72, 4112), (130, 64, 2064), (200, 1000, 1040), (65, 512, 8192), (127, 8, 4096),
                                    # several tiles a CTA, of 192 columns; many slabs; more stages of scales than there are
                                    (2600, 1544, 400), (1300, 2000, 2576), (700, 3000, 4112)])
 def test_product(act, m, n, k):

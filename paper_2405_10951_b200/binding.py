@@ -297,35 +297,60 @@ def bsr_attention_backward(qkv, dout, lse, score_grad=None, use_tensor_cores: bo
 
 # ---- rows of an expert layer, products in 8-bit blocks of 128 -----------------------------------
 # Outputs may be passed in (a decoding loop or a captured graph keeps its buffers); what is not is allocated.  The library sees
-# pointers alone, so types, shapes, contiguity and devices are checked here.
-# A call's checks cost about as much as a small kernel runs, so they are written for few interpreter steps: shapes are compared as
-# tuples, devices as ordinals, and messages are made on refusal only.
-def _run_on(*tensors):
+# pointers alone, so types, shapes, contiguity and devices are checked here.  A call's checks take about as long as a small kernel, so they
+# are written for few interpreter steps: what torch is asked for is kept, and messages are made on refusal only.
+class _Torch:
+    """What the calls below need of torch (imported with the first of them)."""
+
+    def __init__(self):
+        import torch
+        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.i32, self.u8, self.f32, self.bf16, self.e4m3 = torch.int32, torch.uint8, torch.float32, torch.bfloat16, torch.float8_e4m3fn
+        self.device, self.stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+
+
+_torch = None
+
+
+def _th() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
+
+
+def _takes(name, t, dtype, shape):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise BsrError(-1, f"{name} must be a contiguous tensor of {dtype} and shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _takes_codes(T, name, t, shape):
+    """Codes are float8_e4m3fn, or the bytes that hold them."""
+    return _takes(name, t, T.u8 if t.dtype is T.u8 else T.e4m3, shape)
+
+
+def _run_on(T, *tensors):
     """The current stream of the current device, on which all tensors have to be."""
-    import torch
-    ordinal = torch.cuda.current_device()
+    ordinal = T.device()
     for t in tensors:
         if t is not None and t.get_device() != ordinal:
             raise BsrError(-1, f"tensor on {t.device}: the call runs on the current device, cuda:{ordinal}")
-    return torch._C._cuda_getCurrentRawStream(ordinal)
+    return T.stream(ordinal)
 
 
-def _takes(name, t, dtypes, shape):
-    if t.dtype not in dtypes or t.shape != shape or not t.is_contiguous():
-        raise BsrError(-1, f"{name} must be a contiguous tensor of {' or '.join(map(str, dtypes))} and shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
-
-
-def _float_type(name, t):
-    import torch
-    if t.dtype is torch.float32:
-        return DTYPE_FP32
-    if t.dtype is torch.bfloat16:
+def _float_type(T, name, t):
+    if t.dtype is T.bf16:
         return DTYPE_BF16
+    if t.dtype is T.f32:
+        return DTYPE_FP32
     raise BsrError(-1, f"{name} must be float32 or bfloat16, not {t.dtype}")
 
 
-def _at(t):
-    return None if t is None else t.data_ptr()
+def _sizes(name, t, dims):
+    if t.dim() != dims:
+        raise BsrError(-1, f"{name} must have {dims} dimensions, not {t.dim()}")
+    return t.shape
 
 
 def bsr_e4m3_scale_stride(k: int) -> int:
@@ -336,187 +361,155 @@ def bsr_e4m3_scale_stride(k: int) -> int:
 def bsr_expert_sort(expert, experts: int, pos=None, seg_start=None):
     """expert: int32 [tokens, top_k], values outside [0, experts) for slots without an expert.  Returns (pos [tokens, top_k], seg_start
     [experts + 1]) int32."""
-    import torch
-    tokens, top_k = expert.shape
-    _takes("expert", expert, (torch.int32,), (tokens, top_k))
+    T = _th()
+    shape = _sizes("expert", expert, 2)
+    pe = _takes("expert", expert, T.i32, shape)
     if pos is None:
-        pos = torch.empty_like(expert)
+        pos = T.empty_like(expert)
     if seg_start is None:
-        seg_start = torch.empty(max(experts, 0) + 1, dtype=torch.int32, device=expert.device)
-    _takes("pos", pos, (torch.int32,), (tokens, top_k))
-    _takes("seg_start", seg_start, (torch.int32,), (experts + 1,))
-    stream = _run_on(expert, pos, seg_start)
-    _check(lib().bsr_expert_sort(_at(expert), tokens, top_k, experts, _at(pos), _at(seg_start), stream))
+        seg_start = T.empty(max(experts, 0) + 1, dtype=T.i32, device=expert.device)
+    pp, ps = _takes("pos", pos, T.i32, shape), _takes("seg_start", seg_start, T.i32, (experts + 1,))
+    stream = _run_on(T, expert, pos, seg_start)
+    _check((_lib or lib()).bsr_expert_sort(pe, shape[0], shape[1], experts, pp, ps, stream))
     return pos, seg_start
 
 
 def bsr_expert_scatter(x, pos, rows=None):
     """x [tokens, dim] to rows [tokens * top_k, dim] in the order of pos."""
-    import torch
-    tokens, dim = x.shape
-    top_k = pos.shape[1]
-    dt = _float_type("x", x)
+    T = _th()
+    tokens, dim = _sizes("x", x, 2)
+    top_k = _sizes("pos", pos, 2)[1]
+    dt = _float_type(T, "x", x)
     if rows is None:
-        rows = torch.empty((tokens * top_k, dim), dtype=x.dtype, device=x.device)
-    _takes("x", x, (x.dtype,), (tokens, dim))
-    _takes("pos", pos, (torch.int32,), (tokens, top_k))
-    _takes("rows", rows, (x.dtype,), (tokens * top_k, dim))
-    stream = _run_on(x, pos, rows)
-    _check(lib().bsr_expert_scatter(_at(x), dt, tokens, dim, top_k, _at(pos), _at(rows), stream))
+        rows = T.empty((tokens * top_k, dim), dtype=x.dtype, device=x.device)
+    px, pp, pr = _takes("x", x, x.dtype, (tokens, dim)), _takes("pos", pos, T.i32, (tokens, top_k)), _takes("rows", rows, x.dtype, (tokens * top_k, dim))
+    stream = _run_on(T, x, pos, rows)
+    _check((_lib or lib()).bsr_expert_scatter(px, dt, tokens, dim, top_k, pp, pr, stream))
     return rows
 
 
 def bsr_expert_scatter_e4m3(x, pos, q=None, scale=None):
     """The same in E4M3 blocks of 128: returns (codes [tokens * top_k, dim] float8_e4m3fn, scales [tokens * top_k, stride] uint8)."""
-    import torch
-    tokens, dim = x.shape
-    top_k = pos.shape[1]
-    dt = _float_type("x", x)
-    q, scale = _codes_out(x, (tokens * top_k, dim), q, scale)
-    _takes("x", x, (x.dtype,), (tokens, dim))
-    _takes("pos", pos, (torch.int32,), (tokens, top_k))
-    stream = _run_on(x, pos, q, scale)
-    _check(lib().bsr_expert_scatter_e4m3(_at(x), dt, tokens, dim, top_k, _at(pos), _at(q), _at(scale), stream))
+    T = _th()
+    tokens, dim = _sizes("x", x, 2)
+    top_k = _sizes("pos", pos, 2)[1]
+    dt = _float_type(T, "x", x)
+    px, pp = _takes("x", x, x.dtype, (tokens, dim)), _takes("pos", pos, T.i32, (tokens, top_k))
+    q, scale, pq, ps = _codes_out(T, x, (), tokens * top_k, dim, tokens * top_k, q, scale)
+    stream = _run_on(T, x, pos, q, scale)
+    _check((_lib or lib()).bsr_expert_scatter_e4m3(px, dt, tokens, dim, top_k, pp, pq, ps, stream))
     return q, scale
 
 
 def bsr_expert_combine(rows, pos, weights=None, residual=None, out=None, dtype=None):
     """residual + the weighted sum of every token's rows, in the type of out (or of residual, `dtype`, rows).  Without weights and residual: the
     gradient of bsr_expert_scatter."""
-    import torch
-    tokens, top_k = pos.shape
-    dim = rows.shape[1]
+    T = _th()
+    tokens, top_k = _sizes("pos", pos, 2)
+    dim = _sizes("rows", rows, 2)[1]
     if out is None:
-        out = torch.empty((tokens, dim), dtype=residual.dtype if residual is not None else dtype or rows.dtype, device=rows.device)
-    rt, ot = _float_type("rows", rows), _float_type("out", out)
-    _takes("rows", rows, (rows.dtype,), (tokens * top_k, dim))
-    _takes("pos", pos, (torch.int32,), (tokens, top_k))
-    _takes("out", out, (out.dtype,), (tokens, dim))
-    if weights is not None:
-        _takes("weights", weights, (torch.float32,), (tokens, top_k))
-    if residual is not None:
-        _takes("residual", residual, (out.dtype,), (tokens, dim))
-    stream = _run_on(rows, pos, weights, residual, out)
-    _check(lib().bsr_expert_combine(_at(rows), rt, _at(pos), _at(weights), _at(residual), _at(out), ot, tokens, dim, top_k, stream))
+        out = T.empty((tokens, dim), dtype=residual.dtype if residual is not None else dtype or rows.dtype, device=rows.device)
+    rt, ot = _float_type(T, "rows", rows), _float_type(T, "out", out)
+    pr, pp, po = _takes("rows", rows, rows.dtype, (tokens * top_k, dim)), _takes("pos", pos, T.i32, (tokens, top_k)), _takes("out", out, out.dtype, (tokens, dim))
+    pw = None if weights is None else _takes("weights", weights, T.f32, (tokens, top_k))
+    ps = None if residual is None else _takes("residual", residual, out.dtype, (tokens, dim))
+    stream = _run_on(T, rows, pos, weights, residual, out)
+    _check((_lib or lib()).bsr_expert_combine(pr, rt, pp, pw, ps, po, ot, tokens, dim, top_k, stream))
     return out
 
 
 def bsr_expert_combine_backward(dout, rows, pos, weights, drows=None, dw=None):
     """Returns (drows [tokens * top_k, dim] in the type of rows, dw [tokens, top_k] float32)."""
-    import torch
-    tokens, top_k = pos.shape
-    dim = rows.shape[1]
+    T = _th()
+    tokens, top_k = _sizes("pos", pos, 2)
+    dim = _sizes("rows", rows, 2)[1]
     if drows is None:
-        drows = torch.empty_like(rows)
+        drows = T.empty_like(rows)
     if dw is None:
-        dw = torch.empty((tokens, top_k), dtype=torch.float32, device=rows.device)
-    ot, rt = _float_type("dout", dout), _float_type("rows", rows)
-    _takes("dout", dout, (dout.dtype,), (tokens, dim))
-    _takes("rows", rows, (rows.dtype,), (tokens * top_k, dim))
-    _takes("pos", pos, (torch.int32,), (tokens, top_k))
-    _takes("weights", weights, (torch.float32,), (tokens, top_k))
-    _takes("drows", drows, (rows.dtype,), (tokens * top_k, dim))
-    _takes("dw", dw, (torch.float32,), (tokens, top_k))
-    stream = _run_on(dout, rows, pos, weights, drows, dw)
-    _check(lib().bsr_expert_combine_backward(_at(dout), ot, _at(rows), rt, _at(pos), _at(weights), _at(drows), _at(dw), tokens, dim, top_k, stream))
+        dw = T.empty((tokens, top_k), dtype=T.f32, device=rows.device)
+    ot, rt = _float_type(T, "dout", dout), _float_type(T, "rows", rows)
+    pg, pr = _takes("dout", dout, dout.dtype, (tokens, dim)), _takes("rows", rows, rows.dtype, (tokens * top_k, dim))
+    pp, pw = _takes("pos", pos, T.i32, (tokens, top_k)), _takes("weights", weights, T.f32, (tokens, top_k))
+    pd, pdw = _takes("drows", drows, rows.dtype, (tokens * top_k, dim)), _takes("dw", dw, T.f32, (tokens, top_k))
+    stream = _run_on(T, dout, rows, pos, weights, drows, dw)
+    _check((_lib or lib()).bsr_expert_combine_backward(pg, ot, pr, rt, pp, pw, pd, pdw, tokens, dim, top_k, stream))
     return drows, dw
 
 
-def _code_types():
-    import torch
-    return (torch.float8_e4m3fn, torch.uint8)
-
-
-def _codes_out(like, shape, q, scale, name=""):
-    """Codes of `shape` and a row of scales a row (scale_rows: shape[:-1])."""
-    import torch
+def _codes_out(T, like, stack, n, k, scale_rows, q, scale, name=""):
+    """Codes [.., n, k] and their scales [.., scale_rows, stride], made where they are not given; and their addresses."""
+    shape, at = stack + (n, k), stack + (scale_rows, (k + 511) // 512 * 4)
     if q is None:
-        q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=like.device)
-    at = tuple(shape[:-1]) + (bsr_e4m3_scale_stride(shape[-1]),)
+        q = T.empty(shape, dtype=T.e4m3, device=like.device)
     if scale is None:
-        scale = torch.empty(at, dtype=torch.uint8, device=like.device)
-    _takes("codes" + name, q, _code_types(), shape)
-    _takes("scale" + name, scale, (torch.uint8,), at)
-    return q, scale
+        scale = T.empty(at, dtype=T.u8, device=like.device)
+    return q, scale, _takes_codes(T, "codes" + name, q, shape), _takes("scale" + name, scale, T.u8, at)
 
 
 def bsr_quantize_e4m3_rows128(x, q=None, scale=None):
     """x [m, k] to (codes [m, k] float8_e4m3fn, scales [m, stride] uint8)."""
-    m, k = x.shape
-    dt = _float_type("x", x)
-    q, scale = _codes_out(x, (m, k), q, scale)
-    _takes("x", x, (x.dtype,), (m, k))
-    stream = _run_on(x, q, scale)
-    _check(lib().bsr_quantize_e4m3_rows128(_at(x), dt, m, k, _at(q), _at(scale), stream))
+    T = _th()
+    m, k = _sizes("x", x, 2)
+    dt = _float_type(T, "x", x)
+    px = _takes("x", x, x.dtype, (m, k))
+    q, scale, pq, ps = _codes_out(T, x, (), m, k, m, q, scale)
+    stream = _run_on(T, x, q, scale)
+    _check((_lib or lib()).bsr_quantize_e4m3_rows128(px, dt, m, k, pq, ps, stream))
     return q, scale
 
 
 def bsr_quantize_e4m3_blocks128(w, transposed: bool = False, q=None, scale=None, qt=None, scale_t=None):
     """w [n, k] or [count, n, k] to (codes, scales [..., ceil(n / 128), stride]); with `transposed` (or qt and scale_t) also the transposed
     copies [..., k, n] and their scales."""
-    import torch
+    T = _th()
     if w.dim() not in (2, 3):
         raise BsrError(-1, "w must be [n, k] or [count, n, k]")
     n, k = w.shape[-2:]
     stack = tuple(w.shape[:-2])
-    dt = _float_type("w", w)
-    _takes("w", w, (w.dtype,), stack + (n, k))
-
-    def outputs(q, scale, n, k, name=""):
-        at = stack + ((n + 127) // 128, bsr_e4m3_scale_stride(k))
-        if q is None:
-            q = torch.empty(stack + (n, k), dtype=torch.float8_e4m3fn, device=w.device)
-        if scale is None:
-            scale = torch.empty(at, dtype=torch.uint8, device=w.device)
-        _takes("codes" + name, q, _code_types(), stack + (n, k))
-        _takes("scale" + name, scale, (torch.uint8,), at)
-        return q, scale
-
-    q, scale = outputs(q, scale, n, k)
+    dt = _float_type(T, "w", w)
+    pw = _takes("w", w, w.dtype, stack + (n, k))
+    q, scale, pq, ps = _codes_out(T, w, stack, n, k, (n + 127) // 128, q, scale)
+    pqt = pst = None
     if transposed or qt is not None or scale_t is not None:
-        qt, scale_t = outputs(qt, scale_t, k, n, "_t")
-    stream = _run_on(w, q, scale, qt, scale_t)
-    _check(lib().bsr_quantize_e4m3_blocks128(_at(w), dt, stack[0] if stack else 1, n, k, _at(q), _at(scale), _at(qt), _at(scale_t), stream))
+        qt, scale_t, pqt, pst = _codes_out(T, w, stack, k, n, (k + 127) // 128, qt, scale_t, "_t")
+    stream = _run_on(T, w, q, scale, qt, scale_t)
+    _check((_lib or lib()).bsr_quantize_e4m3_blocks128(pw, dt, stack[0] if stack else 1, n, k, pq, ps, pqt, pst, stream))
     return (q, scale) if qt is None else (q, scale, qt, scale_t)
 
 
-def _block128_operands(xq, xs, wq, ws, stack, bias, act, z, y):
-    import torch
-    m, k = xq.shape
+def _block128_operands(T, xq, xs, wq, ws, stack, bias, z, y):
+    """y, the sizes and the addresses in the order of the library's arguments (bias, z and y last)."""
+    m, k = _sizes("xq", xq, 2)
     n = wq.shape[-2]
+    stride = (k + 511) // 512 * 4
     if y is None:
-        y = torch.empty((m, n), dtype=torch.bfloat16, device=xq.device)
-    codes, bf = _code_types(), (torch.bfloat16,)
-    _takes("xq", xq, codes, (m, k))
-    _takes("xs", xs, (torch.uint8,), (m, bsr_e4m3_scale_stride(k)))
-    _takes("wq", wq, codes, stack + (n, k))
-    _takes("ws", ws, (torch.uint8,), stack + ((n + 127) // 128, bsr_e4m3_scale_stride(k)))
-    _takes("y", y, bf, (m, n))
-    if bias is not None:
-        _takes("bias", bias, (torch.float32,), stack + (n,))
-    if z is not None:
-        _takes("z", z, bf, (m, n))
-    return m, n, k, y
+        y = T.empty((m, n), dtype=T.bf16, device=xq.device)
+    at = (_takes_codes(T, "xq", xq, (m, k)), _takes("xs", xs, T.u8, (m, stride)), _takes_codes(T, "wq", wq, stack + (n, k)),
+          _takes("ws", ws, T.u8, stack + ((n + 127) // 128, stride)), None if bias is None else _takes("bias", bias, T.f32, stack + (n,)),
+          None if z is None else _takes("z", z, T.bf16, (m, n)), _takes("y", y, T.bf16, (m, n)))
+    return y, (m, n, k), at
 
 
 def bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, bias=None, act: int = ACT_NONE, z=None, y=None):
     """y [m, n] bf16 = act(x W^T + bias) from the codes and scales of x [m, k] and W [n, k].  act ACT_GELU: the pre-activation goes to z
     [m, n] bf16 if that is given; ACT_GELU_GRAD: the product is multiplied by GELU'(z)."""
-    m, n, k, y = _block128_operands(xq, xs, wq, ws, (), bias, act, z, y)
-    stream = _run_on(xq, xs, wq, ws, bias, z, y)
-    _check(lib().bsr_linear_forward_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(z), _at(y), m, n, k, act, stream))
+    T = _th()
+    _sizes("wq", wq, 2)
+    y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (), bias, z, y)
+    stream = _run_on(T, xq, xs, wq, ws, bias, z, y)
+    _check((_lib or lib()).bsr_linear_forward_e4m3_block128(*at, *sizes, act, stream))
     return y
 
 
 def bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg_start, bias=None, act: int = ACT_NONE, z=None, y=None):
     """The same with a weight per expert: rows seg_start[e] .. seg_start[e + 1] - 1 of x with W[e], wq [experts, n, k], bias [experts, n].  Rows of y and
     z outside every segment stay as they are (a y that is not passed in holds anything there)."""
-    import torch
-    experts = wq.shape[0]
-    m, n, k, y = _block128_operands(xq, xs, wq, ws, (experts,), bias, act, z, y)
-    _takes("seg_start", seg_start, (torch.int32,), (experts + 1,))
-    stream = _run_on(xq, xs, wq, ws, seg_start, bias, z, y)
-    _check(lib().bsr_expert_linear_e4m3_block128(_at(xq), _at(xs), _at(wq), _at(ws), _at(bias), _at(seg_start), _at(z), _at(y), m, n, k, experts, act, stream))
+    T = _th()
+    experts = _sizes("wq", wq, 3)[0]
+    y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (experts,), bias, z, y)
+    pseg = _takes("seg_start", seg_start, T.i32, (experts + 1,))
+    stream = _run_on(T, xq, xs, wq, ws, seg_start, bias, z, y)
+    _check((_lib or lib()).bsr_expert_linear_e4m3_block128(*at[:5], pseg, *at[5:], *sizes, experts, act, stream))
     return y
 
 

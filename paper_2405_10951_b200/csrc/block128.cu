@@ -163,7 +163,7 @@ quantize_blocks128_kernel(const T* __restrict__ w, int n, int k, uint8_t* __rest
   }
 }
 
-int scale_stride128(int k) { return (k + 511) / 512 * 4; }
+int scale_stride128(int k) { return (k / 512 + (k % 512 != 0)) * 4; }
 
 template <typename T>
 static void quantize_rows(const Ctx& c, const void* x, int m, int k, const int* pos, int top_k, void* q, void* scale) {

@@ -218,15 +218,17 @@ struct Scales {
 // GELU(z) = max(z, 0) - |z| Phi(-|z|) and GELU'(z) = Phi(z) + z phi(z), with Phi(-t) = exp(-t^2 / 2) R(t).  R falls from 1/2 and goes as
 // 1 / t: it is u (c1 + c2 u + .. + c5 u^4) in u = 1 / (1 + 0.37677 t), fitted to erfcx in double precision by relative error, 2.9e-5 over
 // 0 <= t <= 14, beyond which the exponential is zero: a hundredth of the rounding to bf16, and of every value, where a polynomial
-// for Phi itself is off by a fixed amount.
-__device__ __forceinline__ void phi_tail2(float z0, float z1, float& p0, float& p1, float& e0, float& e1) {
+// for Phi itself is off by a fixed amount.  t = min(|z|, 16): beyond, the exponential is zero, and so are its products with t, for infinities too.
+__device__ __forceinline__ void phi_tail2(float z0, float z1, float& t0, float& t1, float& p0, float& p1, float& e0, float& e1) {
   const float s = 0.84932180028801907f;                   // sqrt(log2(e) / 2): exp(-z^2 / 2) = 2^-(s z)^2
   float x0, x1, u0, u1;
   unpack2(mul2(pack2(z0, z1), dup2(s)), x0, x1);
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(-x0 * x0));
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(-x1 * x1));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u0) : "f"(fmaf(fabsf(z0), 0.37676923076923075f, 1.0f)));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u1) : "f"(fmaf(fabsf(z1), 0.37676923076923075f, 1.0f)));
+  t0 = fminf(fabsf(z0), 16.f);
+  t1 = fminf(fabsf(z1), 16.f);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u0) : "f"(fmaf(t0, 0.37676923076923075f, 1.0f)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u1) : "f"(fmaf(t1, 0.37676923076923075f, 1.0f)));
   const uint64_t u = pack2(u0, u1);
   uint64_t r = dup2(-0.09088445f);
   r = fma2(r, u, dup2(0.19726645f));
@@ -236,16 +238,16 @@ __device__ __forceinline__ void phi_tail2(float z0, float z1, float& p0, float& 
   unpack2(mul2(mul2(r, u), pack2(e0, e1)), p0, p1);
 }
 __device__ __forceinline__ void gelu2(float& z0, float& z1) {
-  float p0, p1, e0, e1;
-  phi_tail2(z0, z1, p0, p1, e0, e1);
-  z0 = fmaf(-fabsf(z0), p0, fmaxf(z0, 0.f));
-  z1 = fmaf(-fabsf(z1), p1, fmaxf(z1, 0.f));
+  float t0, t1, p0, p1, e0, e1;
+  phi_tail2(z0, z1, t0, t1, p0, p1, e0, e1);
+  z0 = fmaf(-t0, p0, fmaxf(z0, 0.f));
+  z1 = fmaf(-t1, p1, fmaxf(z1, 0.f));
 }
 __device__ __forceinline__ void gelu_grad_mul(float& g0, float& g1, float z0, float z1) {
-  float p0, p1, e0, e1;
-  phi_tail2(z0, z1, p0, p1, e0, e1);
-  g0 *= fmaf(z0 * 0.39894228040143268f, e0, z0 < 0.f ? p0 : 1.f - p0);
-  g1 *= fmaf(z1 * 0.39894228040143268f, e1, z1 < 0.f ? p1 : 1.f - p1);
+  float t0, t1, p0, p1, e0, e1;
+  phi_tail2(z0, z1, t0, t1, p0, p1, e0, e1);
+  g0 *= fmaf(copysignf(t0, z0) * 0.39894228040143268f, e0, z0 < 0.f ? p0 : 1.f - p0);
+  g1 *= fmaf(copysignf(t1, z1) * 0.39894228040143268f, e1, z1 < 0.f ? p1 : 1.f - p1);
 }
 
 struct Out {

@@ -215,7 +215,9 @@ def check(got, zgot, act, part, mag, z, k):
                                    # few tiles: k over 2, 4 and 8 CTAs, shares of rows that do not come out even
                                    (1, 2000, 7168), (7, 72, 4112), (130, 64, 2064), (200, 1000, 1040), (65, 512, 8192), (127, 8, 4096),
                                    # several tiles a CTA, of 192 columns; many slabs; more stages of scales than there are
-                                   (2600, 1544, 400), (1300, 2000, 2576), (700, 3000, 4112)])
+                                   (2600, 1544, 400), (1300, 2000, 2576), (700, 3000, 4112),
+                                   # tiles over two CTAs
+                                   (2600, 1544, 4112), (4200, 776, 5136)])
 def test_product(act, m, n, k):
     import torch
     from paper_2405_10951_b200 import binding as Bd
@@ -235,7 +237,7 @@ def test_product(act, m, n, k):
 @gpu
 @pytest.mark.parametrize("act", [0, 1, 2])
 @pytest.mark.parametrize("counts,n,k", [([1], 64, 128), ([0, 0, 3, 0], 72, 144), ([5, 0, 1, 130, 0, 64], 200, 528), ([0] * 7, 64, 128), ([1] * 64, 264, 512), ([128, 129, 127], 384, 400),
-                                        ([300, 31, 33, 0, 700, 97, 2], 1544, 272), ([2] * 400, 64, 144)])
+                                        ([300, 31, 33, 0, 700, 97, 2], 1544, 272), ([2] * 400, 64, 144), ([1500, 0, 1300, 7, 1290], 1544, 3216)])
 def test_product_per_expert(act, counts, n, k):
     import torch
     from paper_2405_10951_b200 import binding as Bd
@@ -284,6 +286,46 @@ def test_a_row_does_not_depend_on_its_neighbours():
     bad[:40] = 0xff
     y2 = Bd.bsr_expert_linear_e4m3_block128(bad, xs, wq, ws, seg)
     assert torch.equal(y[40:170], y2[40:170]) and bool(torch.isnan(y2[170:]).all())
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(5, 72, 144), (300, 1000, 1040), (2, 512, 4096)])
+def test_scales_far_apart(m, n, k):
+    """Rows and blocks from 2^-100 to 2^100, the least scale (2^-127) among them: a scale is an exponent, nothing of it is lost."""
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    rng = np.random.default_rng(k)
+    far = rng.integers(-100, 101, (m, 1))
+    x = rng.standard_normal((m, k)) * np.ldexp(1.0, far)
+    w = rng.standard_normal((n, k)) / np.sqrt(k)
+    x[0] = np.ldexp(rng.standard_normal(k), -124)
+    w[:min(n, 128)] *= np.ldexp(1.0, 20)
+    t = lambda a: torch.as_tensor(a.astype(np.float32)).cuda()
+    xq, xs = Bd.bsr_quantize_e4m3_rows128(t(x))
+    wq, ws = Bd.bsr_quantize_e4m3_blocks128(t(w))
+    assert int(xs[0, 0]) == 0
+    X, W = P.dequantize(wide(xq), xs.cpu().numpy(), 1), P.dequantize(wide(wq), ws.cpu().numpy(), 128)
+    y = wide(Bd.bsr_linear_forward_e4m3_block128(xq, xs, wq, ws))
+    part, mag = X @ W.T, np.abs(X) @ np.abs(W).T
+    normal = mag > 2.0 ** -100                              # (below, float32 has fewer bits, or flushes)
+    near(y[normal], part[normal], mag[normal], k)
+    assert np.all(np.abs(y[~normal]) <= 2.0 ** -99)
+
+
+@gpu
+@pytest.mark.parametrize("m,k", [(40, 128), (40, 2048), (20000, 128)])
+def test_activations_of_infinities(m, k):
+    """GELU(inf) = inf, GELU(-inf) = 0, GELU'(inf) = 1, GELU'(-inf) = 0, and NaN stays itself: as limits say."""
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    xq, xs, wq, ws, _, _ = operands(np.random.default_rng(k), m, (), 64, k)
+    bias = torch.zeros(64, device="cuda")
+    bias[3], bias[5], bias[7] = float("inf"), float("-inf"), float("nan")
+    y = wide(Bd.bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, bias, act=Bd.ACT_GELU))
+    assert np.all(y[:, 3] == np.inf) and np.all(y[:, 5] == 0) and np.all(np.isnan(y[:, 7])) and np.isfinite(y[:, [0, 1, 2, 4, 6] + list(range(8, 64))]).all()
+    z = bias.bfloat16().expand(m, 64).contiguous()
+    g, plain = (wide(Bd.bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, act=a, z=zz)) for a, zz in [(Bd.ACT_GELU_GRAD, z), (Bd.ACT_NONE, None)])
+    assert np.array_equal(g[:, 3], plain[:, 3]) and np.all(g[:, 5] == 0) and np.all(np.isnan(g[:, 7]))
 
 
 # ---- the layer ------------------------------------------------------------------------------------------------------------

@@ -4,6 +4,7 @@
     python microbench.py backward --m 12800 --n 2304 --k 768
     python microbench.py select_gather --batch 4096 --heads 12 --tokens 197 --dim 768 --keep 0.7
     python microbench.py attention --batch 128 --heads 12 --tokens 197
+    python microbench.py experts --batch 64 --tokens 197 --top-k 2 --experts 16 --dim 384 --hidden 1536
     python microbench.py step --workload vit_b --batch 32 --iters 4
 
 Each prints one JSON line with the time per launch (CUDA events on the current stream, after warm-up) and the
@@ -48,7 +49,7 @@ def timed(fn, iters, flush=None, reps=1):
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("what", choices=["gemm", "backward", "select_gather", "attention", "step"])
+    ap.add_argument("what", choices=["gemm", "backward", "select_gather", "attention", "experts", "step"])
     ap.add_argument("--workload", default="vit_b")
     ap.add_argument("--m", type=int, default=25216)
     ap.add_argument("--n", type=int, default=2304)
@@ -64,6 +65,9 @@ def main():
     ap.add_argument("--dim", type=int, default=768)
     ap.add_argument("--keep", type=float, default=0.7)
     ap.add_argument("--dtype", default="bf16", choices=["bf16", "fp32"])
+    ap.add_argument("--top-k", type=int, default=2)
+    ap.add_argument("--experts", type=int, default=16)
+    ap.add_argument("--hidden", type=int, default=1536)
     ap.add_argument("--flush-l2", action="store_true")
     ap.add_argument("--backward", action="store_true", help="attention: also time the backward pass (--mode 0: without tensor cores)")
     a = ap.parse_args()
@@ -128,6 +132,41 @@ def main():
         gat_bytes = B * ((1 + M) * D * es + (1 + k + 1) * D * es + M * 8)
         out.update(batch=B, heads=H, tokens=T, dim=D, k=k, dtype=a.dtype, select_us=ms_sel * 1e3, select_gbs=sel_bytes / ms_sel / 1e6,
                    gather_us=ms_gat * 1e3, gather_gbs=gat_bytes / ms_gat / 1e6, select_bytes=sel_bytes, gather_bytes=gat_bytes)
+    elif a.what == "experts":
+        # an expert layer with frozen weights in 8-bit blocks, forward and backward, call by call (back-to-back calls of each)
+        M, K, E, D, F = a.batch * a.tokens, a.top_k, a.experts, a.dim, a.hidden
+        expert = torch.topk(torch.randn(M, E, device=dev), K, dim=1)[1].int()
+        wt = torch.softmax(torch.randn(M, K, device=dev), dim=1)
+        x, dout = torch.randn(M, D, device=dev), torch.randn(M, D, device=dev)
+        w1, w2 = (torch.randn(E, F, D, device=dev) / math.sqrt(D)).bfloat16(), (torch.randn(E, D, F, device=dev) / math.sqrt(F)).bfloat16()
+        b1, b2 = torch.randn(E, F, device=dev), torch.randn(E, D, device=dev)
+        W1, W2 = Bd.bsr_quantize_e4m3_blocks128(w1, transposed=True), Bd.bsr_quantize_e4m3_blocks128(w2, transposed=True)
+        pos, seg = Bd.bsr_expert_sort(expert, E)
+        xq, xs = Bd.bsr_expert_scatter_e4m3(x, pos)
+        R = M * K
+        new = lambda n: torch.zeros(R, n, dtype=torch.bfloat16, device=dev)
+        z, h, o, do, dz, dxr, out_t, dx = new(F), new(F), new(D), new(D), new(F), new(D), torch.empty_like(x), torch.empty_like(x)
+        (hq, hs), dw = Bd.bsr_quantize_e4m3_rows128(h), torch.empty_like(wt)
+        (doq, dos), (dzq, dzs) = Bd.bsr_quantize_e4m3_rows128(do), Bd.bsr_quantize_e4m3_rows128(dz)
+        calls = [("sort", lambda: Bd.bsr_expert_sort(expert, E, pos=pos, seg_start=seg)),
+                 ("scatter_e4m3", lambda: Bd.bsr_expert_scatter_e4m3(x, pos, q=xq, scale=xs)),
+                 ("fc1_gelu", lambda: Bd.bsr_expert_linear_e4m3_block128(xq, xs, W1[0], W1[1], seg, b1, act=Bd.ACT_GELU, z=z, y=h)),
+                 ("quantize_hidden", lambda: Bd.bsr_quantize_e4m3_rows128(h, q=hq, scale=hs)),
+                 ("fc2", lambda: Bd.bsr_expert_linear_e4m3_block128(hq, hs, W2[0], W2[1], seg, b2, y=o)),
+                 ("combine", lambda: Bd.bsr_expert_combine(o, pos, wt, residual=x, out=out_t)),
+                 ("combine_backward", lambda: Bd.bsr_expert_combine_backward(dout, o, pos, wt, drows=do, dw=dw)),
+                 ("quantize_dout", lambda: Bd.bsr_quantize_e4m3_rows128(do, q=doq, scale=dos)),
+                 ("fc2_dx_gelu_grad", lambda: Bd.bsr_expert_linear_e4m3_block128(doq, dos, W2[2], W2[3], seg, act=Bd.ACT_GELU_GRAD, z=z, y=dz)),
+                 ("quantize_dz", lambda: Bd.bsr_quantize_e4m3_rows128(dz, q=dzq, scale=dzs)),
+                 ("fc1_dx", lambda: Bd.bsr_expert_linear_e4m3_block128(dzq, dzs, W1[2], W1[3], seg, y=dxr)),
+                 ("combine_dx", lambda: Bd.bsr_expert_combine(dxr, pos, residual=dout, out=dx))]
+        out.update(tokens=M, top_k=K, experts=E, dim=D, hidden=F, us={name: timed(call, a.iters, flush, reps=10) * 1e3 for name, call in calls})
+
+        def layer():
+            for _, call in calls:
+                call()
+        out.update(layer_us=timed(layer, a.iters, flush) * 1e3, layer_tflops=8.0 * R * D * F)
+        out["layer_tflops"] /= out["layer_us"] * 1e6
     else:
         B, H, T = a.batch, a.heads, a.tokens
         qkv = torch.randn(B, T, 3, H, 64, device=dev).bfloat16()

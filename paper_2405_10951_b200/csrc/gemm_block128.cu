@@ -218,36 +218,39 @@ struct Scales {
 // GELU(z) = max(z, 0) - |z| Phi(-|z|) and GELU'(z) = Phi(z) + z phi(z), with Phi(-t) = exp(-t^2 / 2) R(t).  R falls from 1/2 and goes as
 // 1 / t: it is u (c1 + c2 u + .. + c5 u^4) in u = 1 / (1 + 0.37677 t), fitted to erfcx in double precision by relative error, 2.9e-5 over
 // 0 <= t <= 14, beyond which the exponential is zero: a hundredth of the rounding to bf16, and of every value, where a polynomial
-// for Phi itself is off by a fixed amount.  t = min(|z|, 16): beyond, the exponential is zero, and so are its products with t, for infinities too.
-__device__ __forceinline__ void phi_tail2(float z0, float z1, float& t0, float& t1, float& p0, float& p1, float& e0, float& e1) {
-  const float s = 0.84932180028801907f;                   // sqrt(log2(e) / 2): exp(-z^2 / 2) = 2^-(s z)^2
-  float x0, x1, u0, u1;
-  unpack2(mul2(pack2(z0, z1), dup2(s)), x0, x1);
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(-x0 * x0));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(-x1 * x1));
-  t0 = fminf(fabsf(z0), 16.f);
-  t1 = fminf(fabsf(z1), 16.f);
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u0) : "f"(fmaf(t0, 0.37676923076923075f, 1.0f)));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u1) : "f"(fmaf(t1, 0.37676923076923075f, 1.0f)));
+// for Phi itself is off by a fixed amount.  s = -min(|z|, 16): beyond, the exponential is zero, and so are its products with s, for infinities too.
+// Two values at a time, packed wherever an instruction takes pairs (618 -> 541 instructions for 32 rows x 32 columns with the rest: 25216 x 1536 x 384 41.9 -> 37.5 us).
+__device__ __forceinline__ void phi_tail2(uint64_t z, float z0, float z1, uint64_t& s, uint64_t& p, float& e0, float& e1) {
+  float h0, h1, d0, d1, u0, u1;
+  unpack2(mul2(mul2(z, z), dup2(-0.72134752044448170f)), h0, h1);      // exp(-z^2 / 2) = 2^(-log2(e) / 2 z^2)
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(h0));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(h1));
+  s = pack2(fmaxf(-fabsf(z0), -16.f), fmaxf(-fabsf(z1), -16.f));
+  unpack2(fma2(s, dup2(-0.37676923076923075f), dup2(1.0f)), d0, d1);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u0) : "f"(d0));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u1) : "f"(d1));
   const uint64_t u = pack2(u0, u1);
   uint64_t r = dup2(-0.09088445f);
   r = fma2(r, u, dup2(0.19726645f));
   r = fma2(r, u, dup2(0.0858145f));
   r = fma2(r, u, dup2(0.15798381f));
   r = fma2(r, u, dup2(0.14980525f));
-  unpack2(mul2(mul2(r, u), pack2(e0, e1)), p0, p1);
+  p = mul2(mul2(r, u), pack2(e0, e1));
 }
 __device__ __forceinline__ void gelu2(float& z0, float& z1) {
-  float t0, t1, p0, p1, e0, e1;
-  phi_tail2(z0, z1, t0, t1, p0, p1, e0, e1);
-  z0 = fmaf(-t0, p0, fmaxf(z0, 0.f));
-  z1 = fmaf(-t1, p1, fmaxf(z1, 0.f));
+  uint64_t s, p;
+  float e0, e1;
+  phi_tail2(pack2(z0, z1), z0, z1, s, p, e0, e1);
+  unpack2(fma2(s, p, pack2(fmaxf(z0, 0.f), fmaxf(z1, 0.f))), z0, z1);
 }
 __device__ __forceinline__ void gelu_grad_mul(float& g0, float& g1, float z0, float z1) {
-  float t0, t1, p0, p1, e0, e1;
-  phi_tail2(z0, z1, t0, t1, p0, p1, e0, e1);
-  g0 *= fmaf(copysignf(t0, z0) * 0.39894228040143268f, e0, z0 < 0.f ? p0 : 1.f - p0);
-  g1 *= fmaf(copysignf(t1, z1) * 0.39894228040143268f, e1, z1 < 0.f ? p1 : 1.f - p1);
+  uint64_t s, p;
+  float e0, e1, p0, p1, s0, s1;
+  phi_tail2(pack2(z0, z1), z0, z1, s, p, e0, e1);
+  unpack2(p, p0, p1);
+  unpack2(mul2(s, dup2(0.39894228040143268f)), s0, s1);
+  const uint64_t phi = pack2(z0 < 0.f ? p0 : 1.f - p0, z1 < 0.f ? p1 : 1.f - p1);
+  unpack2(mul2(pack2(g0, g1), fma2(pack2(copysignf(s0, z0), copysignf(s1, z1)), pack2(e0, e1), phi)), g0, g1);
 }
 
 struct Out {
@@ -335,6 +338,11 @@ struct Exit {
   }
 };
 
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 // 32 columns of this lane's row of accumulators, with the bias.
 __device__ __forceinline__ void load_sums(uint32_t taddr, const float* sbias, bool bias, float* v) {
   uint32_t r[32];
@@ -346,7 +354,8 @@ __device__ __forceinline__ void load_sums(uint32_t taddr, const float* sbias, bo
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
       const float4 b = *reinterpret_cast<const float4*>(sbias + j);
-      v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+      unpack2(add2(pack2(v[j], v[j + 1]), pack2(b.x, b.y)), v[j], v[j + 1]);
+      unpack2(add2(pack2(v[j + 2], v[j + 3]), pack2(b.z, b.w)), v[j + 2], v[j + 3]);
     }
   }
 }

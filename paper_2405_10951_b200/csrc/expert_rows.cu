@@ -133,7 +133,7 @@ expert_sort_kernel(const int* __restrict__ expert, int slots, int E, int per_war
 // rows[pos[t, s]] = x[t], 16 bytes a thread: x is read once, whatever the number of slots.  A CTA has `cx` chunks of `ty` tokens beside
 // one another, so that a row's bytes leave together (32768 tokens, 8 slots, 2048 wide: a warp walking a token's row 191 us, this
 // 176, the loads of two tokens a thread 180).
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 expert_scatter_kernel(const uint4* __restrict__ x, int tokens, int chunks, int cx, int ty, int top_k, const int* __restrict__ pos, unsigned rows, uint4* __restrict__ out) {
   dependent_sync();
   const int tl = threadIdx.x / cx, ch = blockIdx.y * cx + threadIdx.x - tl * cx, t = blockIdx.x * ty + tl;
@@ -314,15 +314,18 @@ int expert_sort(const Ctx& c, const int* expert, int slots, int E, int* pos, int
   return E <= 16 ? size(std::integral_constant<int, 4>()) : E <= 128 ? size(std::integral_constant<int, 7>()) : size(std::integral_constant<int, 10>());
 }
 
-// A row's chunks over the threads of a CTA: `cx` of them, `ty` tokens beside one another, a row of more than 256 in `parts`.
+// A row's chunks over up to `cap` threads of a CTA: `cx` of them, `ty` tokens beside one another, a row that is too long in `parts`.
 struct Spread {
   int parts, cx, ty, threads;
-  explicit Spread(int chunks) : parts(ceil_div(chunks, 256)), cx(ceil_div(chunks, parts)), ty(256 / cx), threads(ceil_div(cx * ty, 32) * 32) {}
+  Spread(int chunks, int cap) : parts(ceil_div(chunks, cap)), cx(ceil_div(chunks, parts)), ty(cap / cx), threads(ceil_div(cx * ty, 32) * 32) {}
+  bool fuller_than(const Spread& o) const { return (long)cx * ty * o.threads > (long)o.cx * o.ty * threads; }
 };
 
 void expert_scatter(const Ctx& c, const void* x, int tokens, int dim, int top_k, const int* pos, void* rows) {
   const int chunks = (int)(dim * dtype_size(c.dtype) / 16);
-  const Spread s(chunks);
+  // 256 threads, or 512 where that leaves fewer of them without a chunk (6305 tokens, 4 slots, 257 chunks: 129 of 160 threads 26.6 us, 257 of 288
+  // 22.7; in the combination, whose registers then allow fewer CTAs, 32768 tokens, 8 slots, 2048 wide 218 -> 236)
+  const Spread less(chunks, 256), more(chunks, 512), s = more.fuller_than(less) ? more : less;
   note_launch(1);
   launch_k(expert_scatter_kernel, dim3(ceil_div(tokens, s.ty), s.parts), s.threads, 0, c.stream, (const uint4*)x, tokens, chunks, s.cx, s.ty, top_k, pos,
            (unsigned)tokens * (unsigned)top_k, (uint4*)rows);
@@ -330,7 +333,7 @@ void expert_scatter(const Ctx& c, const void* x, int tokens, int dim, int top_k,
 
 template <typename TR, typename TO>
 static void combine(const Ctx& c, const void* rows, const int* pos, const float* w, const void* residual, void* out, int tokens, int dim, int top_k) {
-  const Spread s(dim / Chunk<TR>::N);
+  const Spread s(dim / Chunk<TR>::N, 256);
   auto go = [&](auto kern) {
     note_launch(1);
     launch_k(kern, dim3(ceil_div(tokens, s.ty), s.parts), s.threads, 0, c.stream, (const TR*)rows, pos, w, (const TO*)residual, (TO*)out, tokens, dim, s.cx, s.ty, top_k,
@@ -347,7 +350,12 @@ void expert_combine(const Ctx& c, const void* rows, int rows_dtype, const int* p
 
 template <typename TR, typename TO>
 static void combine_bwd(const Ctx& c, const void* dout, const void* rows, const int* pos, const float* w, void* drows, float* dw, int tokens, int dim, int top_k) {
-  const int chunks = dim / Chunk<TR>::N, wpt = chunks <= 64 ? 1 : chunks <= 128 ? 2 : chunks <= 256 ? 4 : 8;
+  // Warps a token: by the length of its row; fewer where there are tokens enough and the last round would leave most lanes without a
+  // chunk (257 chunks: eight warps 44 us for 6305 tokens and 4 slots of floats, one 41).
+  const int chunks = dim / Chunk<TR>::N;
+  int wpt = chunks <= 64 ? 1 : chunks <= 128 ? 2 : chunks <= 256 ? 4 : 8;
+  auto lanes = [&](int w) { return 32 * w * ceil_div(chunks, 32 * w); };
+  while (wpt > 1 && (long)tokens * wpt >= 32 * B200_SMS && lanes(wpt) * 9 > lanes(1) * 10) wpt /= 2;
   auto go = [&](auto kern) {
     note_launch(1);
     launch_k(kern, ceil_div(tokens, 8 / wpt), 256, 0, c.stream, (const TO*)dout, (const TR*)rows, pos, w, (TR*)drows, dw, tokens, dim, wpt, top_k, (unsigned)tokens * (unsigned)top_k);

@@ -261,6 +261,39 @@ def test_product_per_expert(act, counts, n, k):
 
 
 @gpu
+@pytest.mark.parametrize("m,n,k,experts", [(620000, 8, 16, 0), (9000, 1544, 16, 1024), (160000, 776, 768, 0), (170000, 776, 768, 5), (5000, 776, 4112, 3)])
+def test_many_tiles_a_worker(m, n, k, experts):
+    """More tiles a CTA, or pair of them, than its list holds; the last case: segments of no rows at all.  Rows are compared by sample."""
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    rng = np.random.default_rng(n)
+    x = (torch.randn((m, k), device="cuda") * torch.exp2(torch.randint(-6, 7, (m, 1), device="cuda").float())).bfloat16()
+    w = (torch.randn((max(experts, 1), n, k), device="cuda") / np.sqrt(k)).bfloat16()
+    xq, xs = Bd.bsr_quantize_e4m3_rows128(x)
+    wq, ws = Bd.bsr_quantize_e4m3_blocks128(w)
+    ends = np.zeros(experts + 1, np.int32)
+    if experts and m != 5000:
+        ends[1:] = np.sort(rng.integers(0, m - 50, experts))
+        ends[1:4] = ends[3]                               # two experts without rows
+    y0 = torch.full((m, n), 7.0, dtype=torch.bfloat16, device="cuda")
+    if experts:
+        y = Bd.bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, torch.as_tensor(ends).cuda(), y=y0.clone())
+    else:
+        y = Bd.bsr_linear_forward_e4m3_block128(xq, xs, wq[0], ws[0], y=y0.clone())
+    pick = np.unique(np.concatenate([np.arange(0, m, m // 700), np.arange(m - 300, m), ends[:-1], np.maximum(ends - 1, 0)]))
+    at = torch.as_tensor(pick).cuda()
+    X, Y = P.dequantize(wide(xq[at]), xs[at].cpu().numpy(), 1), wide(y[at])
+    of = np.searchsorted(ends[1:], pick, side="right") if experts else np.zeros(len(pick), int)
+    for e in np.unique(of):
+        rows = of == e
+        if experts and e == experts:
+            assert np.all(Y[rows] == 7.0)
+            continue
+        W = P.dequantize(wide(wq[e]), ws[e].cpu().numpy(), 128)
+        near(Y[rows], X[rows] @ W.T, np.abs(X[rows]) @ np.abs(W).T, k)
+
+
+@gpu
 def test_segments_outside_the_rows_are_cut():
     import torch
     from paper_2405_10951_b200 import binding as Bd

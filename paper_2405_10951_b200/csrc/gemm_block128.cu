@@ -3,7 +3,8 @@
 //   y[m, n] = act( sum_b 2^(ea[m, b] + ew[n / 128, b]) sum_{k in block b} Aq(m, k) Wq(n, k) + bias[n] )
 //
 // dense, or over rows sorted by expert with a weight matrix per expert (rows seg_start[e] .. seg_start[e + 1] use matrix e; an
-// expert's tiles begin at its first row, and what a tile's last rows hold of the next expert is never stored).
+// expert's tiles begin at its first row, and what a tile's last rows hold of the next expert is never stored).  A row's sums do not depend
+// on its neighbours.
 //
 // tcgen05.mma kind::mxf8f6f4 multiplies each 32 values of k by one scale a row of A and one a row of W, read from tensor memory as
 // the byte e + 127 that the scales are held in.  A word of tensor memory has four such bytes, and an instruction says which one it
@@ -11,10 +12,14 @@
 // cost one copy of 512 bytes a 128 rows and four slabs.  (Scaling the partial sums of every slab in registers instead would read the
 // accumulators once a slab.)
 //
-// Two kernels, both persistent, a tile's rows spread over warps in the same way:
-//   gemm_block128_kernel       one CTA a tile of 128 rows and 64, 128 or 192 columns (two accumulators of 192 leave tensor memory for
-//                              the scales; two of 256 would not)
-//   gemm_block128_pair_kernel  two CTAs (cta_group::2) a tile of 256 rows and up to 240 columns
+// Three kernels:
+//   gemm_block128_kernel        persistent, one CTA a tile of 128 rows and 64, 128 or 192 columns (two accumulators of 192 leave tensor memory
+//                               for the scales; two of 256 would not)
+//   gemm_block128_pair_kernel   persistent, two CTAs (cta_group::2) a tile of 256 rows and up to 240 columns: long k, many rows
+//   gemm_block128_small_kernel  a tile's k over the CTAs of a cluster: few tiles
+// What bounds them: the tensor pipe where k is long (8192 x 4096 x 7168: busy 84 % of 179 us, 2.68 PFLOP/s; under the power limit 207 us); at k = 768 and below what
+// operand loads, output stores and the tensor core's reads share inside an SM (25216 x 2304 x 768 51.5 us, without stores 45, without an epilogue 39).
+// The persistent kernels' warps:
 //   warp 0      : TMA producer (one lane)
 //   warp 1      : tensor-memory allocation, copies of scales to tensor memory, MMA issue (one lane)
 //   warp 2      : scales from global to shared memory, in the order in which tensor memory takes them
@@ -644,9 +649,8 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 
 // ---- two CTAs a tile -------------------------------------------------------------------------------------------------------
 // As gemm_tc2.cu: each SM stages its own 128 rows of A and half of the columns of W, 31 KB a slab for 256 x 240 sums where one CTA
-// takes 40 KB for 128 x 192: the L2-to-SM path bounds both (about 50 bytes a clock and SM).  Both CTAs hold the scales of their own rows and of
-// all columns.  `width` columns a tile, a multiple of 16, is chosen for each product: up to 240, so that two accumulators and two turns
-// of scales fit tensor memory.
+// takes 40 KB for 128 x 192.  Both CTAs hold the scales of their own rows and of all columns.  `width` columns a tile, a multiple of 16, is chosen
+// for each product: up to 240, so that two accumulators and two turns of scales fit tensor memory.  Four, five or six stages: within 3 %.
 constexpr int P_WIDTH = 240, P_STAGES = 5, P_BIAS_BYTES = 128 * 4;
 constexpr int P_STAGE_BYTES = A_BYTES + P_WIDTH / 2 * BK;
 constexpr int P_SMEM_BYTES = P_STAGES * P_STAGE_BYTES + EPI_WARPS * (STAGING_BYTES + P_BIAS_BYTES) + SF_STAGES * SF_BYTES + 1024;
@@ -1110,7 +1114,7 @@ static bool make_out_map(CUtensorMap* map, const void* ptr, int n, int m, int co
             cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Width of a pair's tiles: the number of waves times what a slab of such a tile takes (its bytes at 50 a clock and SM).
+// Width of a pair's tiles: the number of waves times what a slab of such a tile takes (160, 192, 240 columns: 341, 370, 402 ns).
 static int pair_width(long tiles_m, int n, int pairs) {
   int best = P_WIDTH;
   double t_best = 1e30;

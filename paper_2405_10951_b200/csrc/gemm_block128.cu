@@ -3,8 +3,8 @@
 //   y[m, n] = act( sum_b 2^(ea[m, b] + ew[n / 128, b]) sum_{k in block b} Aq(m, k) Wq(n, k) + bias[n] )
 //
 // dense, or over rows sorted by expert with a weight matrix per expert (rows seg_start[e] .. seg_start[e + 1] use matrix e; an
-// expert's tiles begin at its first row, and what a tile's last rows hold of the next expert is never stored).  A row's sums do not depend
-// on its neighbours.
+// expert's tiles begin at its first row, and what a tile's last rows hold of the next expert is never stored).  Over
+// sorted rows a row's sums do not depend on the others: k is never cut there, as it is for a dense product of few rows.
 //
 // tcgen05.mma kind::mxf8f6f4 multiplies each 32 values of k by one scale a row of A and one a row of W, read from tensor memory as
 // the byte e + 127 that the scales are held in.  A word of tensor memory has four such bytes, and an instruction says which one it
@@ -879,7 +879,7 @@ constexpr uint32_t S_TMEM_COLS = 128, S_SF_COL = S_BN;
 constexpr int S_PASSES = BM / 2 / 16;                                  // a CTA finishes 16 rows a pass
 
 template <int ACT>
-__global__ void __launch_bounds__(S_THREADS)
+__global__ void __launch_bounds__(S_THREADS, 1)
 gemm_block128_small_kernel(const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w, Problem p, Out out, int* status) {
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bar_mem[2 * S_STAGES + 2 * SF_STAGES + 1];

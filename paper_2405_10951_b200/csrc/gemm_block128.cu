@@ -43,8 +43,7 @@ constexpr int BM = 128, BK = 128, UMMA_K = 32;             // a slab is a block 
 constexpr int A_BYTES = BM * BK;
 constexpr int SF_BYTES = 3 * 512;                          // words of 128 rows of A, of up to 256 rows of W
 constexpr int EPI_WARPS = 12, EPI_SHARE = EPI_WARPS / 4;   // warps that share a quarter's chunks of columns
-// Scales wait in SF_STAGES stages of shared memory (their way there is long beside a group of few slabs) and go to tensor memory in turns
-// of two: the copy of a group's into the place of those before the last waits until the products that read these are done.
+// Scales wait in SF_STAGES stages of shared memory: their way there is long beside a group of few slabs.
 constexpr int SF_STAGES = 4;
 constexpr int STAGING_BYTES = 4096;                        // a warp's 32 rows x 64 columns of bf16
 constexpr int THREADS = 96 + EPI_WARPS * 32;
@@ -464,7 +463,7 @@ constexpr int RING_BYTES = 160 * 1024;
 constexpr int stages_for(int bn) { return RING_BYTES / (A_BYTES + bn * BK) < 8 ? RING_BYTES / (A_BYTES + bn * BK) : 8; }
 constexpr int BIAS_BYTES = 64 * 4;   // bias of a warp's columns of a tile: 192 among three
 constexpr int SMEM_BYTES = RING_BYTES + EPI_WARPS * (STAGING_BYTES + BIAS_BYTES) + SF_STAGES * SF_BYTES + 1024;
-constexpr uint32_t SF_COL = 384;     // four columns of A's scales and eight of W's per turn, 16 apart
+constexpr uint32_t SF_COL = 384;     // four columns of A's scales and eight of W's per stage, 16 apart
 
 template <int BN, int ACT>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -558,10 +557,9 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + buf * BN;
         for (int kb = 0; kb < total_kb; ++kb) {
-          const uint32_t sfa = tmem_base + SF_COL + (sf & 1) * 16, sfb = sfa + 4;
+          const uint32_t sfa = tmem_base + SF_COL + sf * 16, sfb = sfa + 4;
           if ((kb & 3) == 0) {
-            // (stage sf - 2's barrier: the last time it was there to be emptied, by this turn's products before)
-            if (!mbar_wait(sempty_bar(sf ^ 2), sf < 2 ? sphase ^ 1u : sphase, abortp) || !mbar_wait(sfull_bar(sf), sphase, abortp)) { ok = false; break; }
+            if (!mbar_wait(sfull_bar(sf), sphase, abortp)) { ok = false; break; }
             tc_fence_after();
             const uint64_t ds = desc_s0 + (uint64_t)((sf * SF_BYTES) >> 4);
             copy_scales(sfa, ds);
@@ -650,7 +648,8 @@ gemm_block128_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 // ---- two CTAs a tile -------------------------------------------------------------------------------------------------------
 // As gemm_tc2.cu: each SM stages its own 128 rows of A and half of the columns of W, 31 KB a slab for 256 x 240 sums where one CTA
 // takes 40 KB for 128 x 192.  Both CTAs hold the scales of their own rows and of all columns.  `width` columns a tile, a multiple of 16, is chosen
-// for each product: up to 240, so that two accumulators and two turns of scales fit tensor memory.  Four, five or six stages: within 3 %.
+// for each product: up to 240, so that two accumulators and the scales of two groups fit tensor memory; a group's are copied into the place of those
+// before the last once the products that read these are done.  Four, five or six stages: within 3 %.
 constexpr int P_WIDTH = 240, P_STAGES = 5, P_BIAS_BYTES = 128 * 4;
 constexpr int P_STAGE_BYTES = A_BYTES + P_WIDTH / 2 * BK;
 constexpr int P_SMEM_BYTES = P_STAGES * P_STAGE_BYTES + EPI_WARPS * (STAGING_BYTES + P_BIAS_BYTES) + SF_STAGES * SF_BYTES + 1024;

@@ -1113,25 +1113,30 @@ static bool make_out_map(CUtensorMap* map, const void* ptr, int n, int m, int co
             cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Width of a pair's tiles: the number of waves times what a slab of such a tile takes (160, 192, 240 columns: 341, 370, 402 ns).
-static int pair_width(long tiles_m, int n, int pairs) {
-  int best = P_WIDTH;
-  double t_best = 1e30;
+// How a product that is not of few tiles is cut: what fits the SMs in one wave takes the narrowest tiles that do; else one CTA or two a tile,
+// and the pair's width, by waves times the time of one.  A wave takes 0.93 us and 0.367 a slab on single CTAs, 1.5 and 0.38 on pairs of 240 columns
+// (narrower ones less: a slab of 160, 192, 240 columns 341, 370, 402 ns where nothing else waits), or, longer, its epilogue (by activation).
+//   us of a launch, one CTA a tile and two:
+//   25216 x 2304 x 384    32.6 / 35.6      25216 x 2304 x 768    50.3 / 51.2      25216 x 2304 x 1536   85.5 / 80.0      6304 x 2304 x 768    16.0 / 17.7
+//   25216 x 768 x 1536    29.5 / 34.9      2048 x 2048 x 4096    22.8 / 17.8      3000 x 1000 x 7168    20.3 / 24.4      4096 x 4096 x 4096   57.0 / 52.7
+//   8192 x 4096 x 7168     193 / 177       8192 x 1024 x 1024    13.5 / 15.8      64 experts of 768 rows, 1408 x 2048: 150 / 133
+//   16 experts, 25216 x 1536 x 768 with GELU: 49.5 / 54.2
+// Experts are taken to have equal shares of the rows (their counts are on the device).
+struct Cut { bool pair; int bn; };
+static Cut choose_cut(int m, int n, int k, int experts, int act, int sms) {
+  const int share = ceil_div(m, experts), kb = ceil_div(k, BK);
+  auto tiles = [&](int rows, int cols) { return (long)(experts < m ? experts : m) * ceil_div(share, rows) * ceil_div(n, cols); };
+  if (n <= 64 || tiles(BM, 64) <= sms) return {false, 64};
+  if (n <= 128 || tiles(BM, 128) <= sms) return {false, 128};
+  auto longer = [](double x, double y) { return x > y ? x : y; };
+  const double epi1[3] = {0.0, 3.3, 4.3}, epi2[3] = {0.0, 4.6, 5.3};
+  Cut best = {false, 192};
+  double t_best = ceil_div(tiles(BM, 192), sms) * longer(0.93 + 0.367 * kb, epi1[act]);
   for (int w = P_WIDTH; w >= 128; w -= 16) {
-    const double t = (double)((tiles_m * ceil_div(n, w) + pairs - 1) / pairs) * (BM + w / 2 + 24);
-    if (t < t_best) { t_best = t; best = w; }
+    const double t = ceil_div(tiles(2 * BM, w), sms / 2) * longer(1.5 + 0.38 * kb * (152 + w / 2) / 272, epi2[act]);
+    if (t < t_best) { t_best = t; best = {true, w}; }
   }
   return best;
-}
-
-// us of a launch in a row of launches, one CTA a tile and two:
-//   25216 x 2304 x 384    34.5 / 37.0      25216 x 2304 x 768    54.9 / 51.5      25216 x 2304 x 1536   88 / 82       6304 x 2304 x 768    17.7 / 18.7
-//   25216 x 384 x 1536    18.1 / 20.2      4096 x 4096 x 4096    59.2 / 53.2      8192 x 4096 x 7168    203 / 179
-// Two take fewer bytes a slab but longer to fill and drain, so they want a long k, several waves and columns for wide tiles; and rows: an
-// expert's last tile is half empty on average.
-static bool use_pairs(int m, int n, int k, int experts, int sms) {
-  const long tiles = (long)ceil_div(m, 2 * BM) * ceil_div(n, P_WIDTH);
-  return k >= 768 && n >= 768 && m / experts >= 512 && tiles * k >= 2l * sms * 1024;
 }
 
 }  // namespace tcb
@@ -1142,10 +1147,10 @@ int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void*
   using namespace tcb;
   const int sms = c.sm_count > 0 ? c.sm_count : B200_SMS;
   const long some = seg_start != nullptr ? (experts < m ? experts : m) - 1 : 0;      // at most so many tiles more than the rows alone would take
-  const long tiles_m = ceil_div(m, BM) + some;
   const int splits = seg_start == nullptr ? small_splits(m, n, k, sms) : 0;
-  const bool pair = splits == 0 && use_pairs(m, n, k, experts, sms);
-  const int bn = splits > 0 ? S_BN : pair ? pair_width(ceil_div(m, 2 * BM) + some / 2, n, sms / 2) : tiles_m * ceil_div(n, 64) <= sms ? 64 : tiles_m * ceil_div(n, 128) <= sms ? 128 : 192;
+  const Cut cut = splits > 0 ? Cut{false, S_BN} : choose_cut(m, n, k, experts, e.act, sms);
+  const bool pair = cut.pair;
+  const int bn = cut.bn;
   bf16* z = (bf16*)(e.act == 1 ? e.aux_out : const_cast<void*>(e.aux_in));
   CUtensorMap ma, ma32, mw, my, mz;
   if (!make_out_map(&my, C, n, m, chunk_of(e.act)) || !make_out_map(&mz, z != nullptr ? z : C, n, m, chunk_of(e.act))) return -2;
@@ -1160,7 +1165,7 @@ int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void*
   o.z = z;
   o.bias = e.bias;
   o.release = false;
-  const long tiles = (pair ? ceil_div(m, 2 * BM) + some : tiles_m) * p.tiles_n;
+  const long tiles = (ceil_div(m, pair ? 2 * BM : BM) + some) * p.tiles_n;
   auto go = [&](auto act) {
     constexpr int A = decltype(act)::value;
     if (splits > 0) return launch_small<A>(c, ma32, mw, p, o, splits);

@@ -24,7 +24,7 @@ def test_refusals():
                 dict(q=O), dict(qt=O, st=A)]:
         a = dict(w=A, dt=0, c=2, n=32, k=32, q=A, s=A, qt=None, st=None) | bad
         refused("bsr_quantize_e4m3_blocks128", a["w"], a["dt"], a["c"], a["n"], a["k"], a["q"], a["s"], a["qt"], a["st"], None)
-    for bad in [dict(x=None), dict(x=O), dict(w=None), dict(xs=None), dict(ws=4098), dict(b=O), dict(y=None), dict(y=O), dict(m=-1), dict(n=4), dict(n=12), dict(k=8), dict(act=3), dict(act=-1),
+    for bad in [dict(x=None), dict(x=O), dict(w=None), dict(xs=None), dict(ws=4098), dict(b=O), dict(y=None), dict(y=O), dict(m=-1), dict(m=(1 << 30) + 1), dict(n=(1 << 30) + 8), dict(k=(1 << 30) + 16), dict(n=4), dict(n=12), dict(k=8), dict(act=3), dict(act=-1),
                 dict(act=0, z=A), dict(act=2, z=None), dict(act=1, z=O)]:
         a = dict(x=A, xs=A, w=A, ws=A, b=A, z=None, y=A, m=4, n=16, k=32, act=0) | bad
         refused("bsr_linear_forward_e4m3_block128", a["x"], a["xs"], a["w"], a["ws"], a["b"], a["z"], a["y"], a["m"], a["n"], a["k"], a["act"], None)

@@ -487,6 +487,68 @@ def test_expert_layer_on_another_stream_and_in_a_graph():
         assert torch.equal(on_side[k], want_a[k]), k
 
 
+def large_calls(Bd, a):
+    """A sort over a cluster of sixteen CTAs, rows in blocks, a product over pairs of CTAs, one over a cluster, the weighted sum."""
+    import torch
+    pos, seg = Bd.bsr_expert_sort(a["expert"], 12)
+    q, s = Bd.bsr_expert_scatter_e4m3(a["x"], pos, q=torch.zeros((a["expert"].numel(), 272), dtype=torch.uint8, device="cuda"), scale=torch.zeros((a["expert"].numel(), 4), dtype=torch.uint8, device="cuda"))
+    y = Bd.bsr_linear_forward_e4m3_block128(a["xq"], a["xs"], a["wq"], a["ws"])
+    few = Bd.bsr_linear_forward_e4m3_block128(a["xq"][:40], a["xs"][:40], a["wq"], a["ws"], act=Bd.ACT_GELU)
+    out = Bd.bsr_expert_combine(a["rows"], pos, a["weights"])
+    return [pos, seg, q, s, y, few, out]
+
+
+def large_inputs(seed):
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    rng = np.random.default_rng(seed)
+    expert, weights = P.routing(rng, 17000, 5, 12, masked=0.1)
+    torch.manual_seed(seed)
+    a = dict(expert=torch.as_tensor(expert).cuda(), weights=torch.as_tensor(weights).cuda(), x=torch.randn((17000, 272), device="cuda"), rows=torch.randn((85000, 272), device="cuda").bfloat16())
+    a["xq"], a["xs"] = Bd.bsr_quantize_e4m3_rows128(torch.randn((2600, 4112), device="cuda"))
+    a["wq"], a["ws"] = Bd.bsr_quantize_e4m3_blocks128(torch.randn((1544, 4112), device="cuda"))
+    return a
+
+
+@gpu
+def test_large_calls_captured_and_replayed():
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    a, b = large_inputs(1), large_inputs(2)
+    want = [[t.clone() for t in large_calls(Bd, v)] for v in (a, b)]
+    held = {k: v.clone() for k, v in a.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = large_calls(Bd, held)
+    for inputs, expected in [(a, want[0]), (b, want[1]), (a, want[0])]:
+        for k, v in inputs.items():
+            held[k].view(torch.uint8).copy_(v.view(torch.uint8))
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(got, expected):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@gpu
+def test_calls_on_two_streams_at_once():
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    inputs = [large_inputs(3), large_inputs(4)]
+    want = [[t.clone() for t in large_calls(Bd, v)] for v in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(5):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(large_calls(Bd, inputs[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for outs in got[i]:
+            for x, y in zip(outs, want[i]):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
 @gpu
 def test_long_offsets():
     """More than 2^31 values of an operand: offsets pass 32 bits."""

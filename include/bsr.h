@@ -410,7 +410,8 @@ int32_t bsr_expert_sort(const int32_t* expert_dev, int32_t tokens, int32_t top_k
 
 /* rows[pos[t, s]] = x[t] for every slot that has a row.  x [tokens, dim] and rows_dev_out [tokens * top_k, dim] in `dtype`;
  * pos as bsr_expert_sort writes it (a position outside the rows counts as none); rows behind the last one stay as they
- * were.  dim * sizeof(dtype) must be a multiple of 16.  The gradient of x is bsr_expert_combine without weights and residual. */
+ * were.  dim * sizeof(dtype) must be a multiple of 16, dim at most 2^25 (here, in the combination and in its gradient).  The gradient of x is
+ * bsr_expert_combine without weights and residual. */
 int32_t bsr_expert_scatter(const void* x_dev, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos_dev,
                            void* rows_dev_out, void* stream);
 /* The same with the rows in E4M3 blocks: codes_dev_out [tokens * top_k, dim] and scale_dev_out [tokens * top_k,

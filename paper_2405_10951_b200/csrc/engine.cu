@@ -1794,12 +1794,15 @@ static bool unaligned(std::initializer_list<const void*> ps, uintptr_t to = 16) 
   return false;
 }
 static bool bad_dtype(int32_t d) { return d != BSR_DTYPE_FP32 && d != BSR_DTYPE_BF16; }
+// A row's parts lie along the grid's second axis, and a lane's column is a 32-bit number that its last step must not take past 2^31.
+constexpr int32_t LONGEST_ROW = 1 << 25;
 // Sizes that the calls on (token, slot) pairs share; rows of `dtype` are whole 16-byte units.
 static int check_slots(int32_t tokens, int32_t dim, int32_t top_k, int32_t dtype) {
   if (tokens < 0 || top_k < 1 || (int64_t)tokens * top_k > (1 << 30)) return set_err(g_error, BSR_ERR_INVALID_ARG, "need tokens >= 0, top_k >= 1 and tokens * top_k <= 2^30");
   if (dim < 1 || (dim * dtype_size(dtype)) % 16 != 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad shape: rows must be a multiple of 16 bytes");
   return BSR_OK;
 }
+static int check_row(int32_t dim) { return dim > LONGEST_ROW ? set_err(g_error, BSR_ERR_INVALID_ARG, "dim must be at most 2^25") : BSR_OK; }
 
 // The kernels number blocks of 128 with 32 bits.
 static bool few_blocks(int64_t m, int64_t k) { return m * ((k + 127) / 128) < (int64_t)UINT32_MAX - 65535; }
@@ -1818,6 +1821,7 @@ int32_t bsr_expert_sort(const int32_t* expert, int32_t tokens, int32_t top_k, in
 int32_t bsr_expert_scatter(const void* x, int32_t dtype, int32_t tokens, int32_t dim, int32_t top_k, const int32_t* pos, void* rows, void* stream) {
   if (bad_dtype(dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
   if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
+  if (int rc = check_row(dim)) return rc;
   if (tokens == 0) return BSR_OK;
   if (x == nullptr || pos == nullptr || rows == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   if (unaligned({x, rows})) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned");
@@ -1842,6 +1846,7 @@ int32_t bsr_expert_combine(const void* rows, int32_t rows_dtype, const int32_t* 
   if (bad_dtype(dtype) || bad_dtype(rows_dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
   if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
   if (int rc = check_slots(tokens, dim, top_k, rows_dtype)) return rc;
+  if (int rc = check_row(dim)) return rc;
   if (tokens == 0) return BSR_OK;
   if (rows == nullptr || pos == nullptr || out == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   if (unaligned({rows, residual, out})) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned");
@@ -1854,6 +1859,7 @@ int32_t bsr_expert_combine_backward(const void* dout, int32_t dtype, const void*
   if (bad_dtype(dtype) || bad_dtype(rows_dtype)) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad dtype");
   if (int rc = check_slots(tokens, dim, top_k, dtype)) return rc;
   if (int rc = check_slots(tokens, dim, top_k, rows_dtype)) return rc;
+  if (int rc = check_row(dim)) return rc;
   if (tokens == 0) return BSR_OK;
   if (dout == nullptr || rows == nullptr || pos == nullptr || weights == nullptr || drows == nullptr || dweights == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   if (unaligned({dout, rows, drows})) return set_err(g_error, BSR_ERR_INVALID_ARG, "rows must be 16-byte aligned");

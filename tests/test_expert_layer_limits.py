@@ -1,0 +1,27 @@
+"""Sizes that the calls of an expert layer refuse.  Nothing of these calls reaches a device."""
+import pytest
+
+A = 4096                     # an aligned address, never read: the arguments are checked first
+
+
+def status(name, *args):
+    from paper_2405_10951_b200 import binding as Bd
+    return getattr(Bd.lib(), name)(*args)
+
+
+@pytest.mark.parametrize("dim", [(1 << 25) + 16, 1 << 26, (1 << 31) - 16])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_rows_too_long_for_a_grid_are_refused(dtype, dim):
+    """A row's parts lie along the grid's second axis (65535 at most), and a lane walks its columns in 32 bits: within 2048 of 2^31 the
+    combination's gradient would step past the end to negative columns."""
+    assert status("bsr_expert_scatter", A, dtype, 1, dim, 1, A, A, None) == -1
+    assert status("bsr_expert_combine", A, dtype, A, A, A, A, 1 - dtype, 1, dim, 1, None) == -1
+    assert status("bsr_expert_combine_backward", A, dtype, A, 1 - dtype, A, A, A, A, 1, dim, 1, None) == -1
+
+
+@pytest.mark.parametrize("chunk,threads", [(4, 1024), (8, 2048)])
+def test_the_longest_row_fits(chunk, threads):
+    """The kernels' own arithmetic at the longest row: parts of at most 256 chunks, columns of the last step of eight warps."""
+    chunks = -(-(1 << 25) // chunk)
+    assert -(-chunks // 256) <= 65535
+    assert (1 << 25) + threads < 1 << 31

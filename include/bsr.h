@@ -442,8 +442,8 @@ int32_t bsr_quantize_e4m3_blocks128(const void* w_dev, int32_t dtype, int32_t co
                                     void* codes_t_dev_out, void* scale_t_dev_out, void* stream);
 
 /* y = act(x W^T + bias) of such operands, accumulated in float32.  x [m, k], w [n, k], bias [n] float32 or NULL, y [m, n]
- * bf16; k a multiple of 16, n of 8, m, n and k at most 2^30.  act: BSR_ACT_NONE (z NULL); BSR_ACT_GELU, with the pre-activation written to z [m, n] bf16 unless
- * it is NULL; BSR_ACT_GELU_GRAD: x W^T + bias times GELU'(z), z read. */
+ * bf16; k a multiple of 16 and at most 2^24, n of 8, m and n at most 2^30.  act: BSR_ACT_NONE (z NULL); BSR_ACT_GELU, with the pre-activation written to
+ * z [m, n] bf16 unless it is NULL; BSR_ACT_GELU_GRAD: x W^T + bias times GELU'(z), z read. */
 enum { BSR_ACT_NONE = 0, BSR_ACT_GELU = 1, BSR_ACT_GELU_GRAD = 2 };
 int32_t bsr_linear_forward_e4m3_block128(const void* x_codes_dev, const void* x_scale_dev, const void* w_codes_dev, const void* w_scale_dev,
                                          const float* bias_dev, void* z_dev, void* y_dev, int32_t m, int32_t n, int32_t k, int32_t act,

@@ -1890,10 +1890,11 @@ int32_t bsr_quantize_e4m3_blocks128(const void* w, int32_t dtype, int32_t count,
 
 static int32_t linear_block128(const char* what, const void* x, const void* xs, const void* w, const void* ws, const float* bias, const int32_t* seg_start, void* z, void* y,
                                int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, void* stream) {
-  // sizes that a round up to a tile keeps within 31 bits
-  constexpr int32_t LARGEST = 1 << 30;
-  if (m < 0 || n < 8 || n % 8 != 0 || k < 16 || k % 16 != 0 || m > LARGEST || n > LARGEST || k > LARGEST)
-    return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0, n a multiple of 8 and k a multiple of 16, each at most 2^30");
+  // Sizes that a round up to a tile keeps within 31 bits; sums that end long before a wait for them does (a slab of 128 values takes a CTA
+  // about 0.37 us, so 2^24 values 48 ms of the two seconds that a wait may last; and their accumulator drops a 16th of them at most).
+  constexpr int32_t LARGEST = 1 << 30, LONGEST_SUM = 1 << 24;
+  if (m < 0 || n < 8 || n % 8 != 0 || k < 16 || k % 16 != 0 || m > LARGEST || n > LARGEST || k > LONGEST_SUM)
+    return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0, n a multiple of 8, each at most 2^30, and k a multiple of 16 up to 2^24");
   if (act < BSR_ACT_NONE || act > BSR_ACT_GELU_GRAD) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad act");
   if (m == 0) return BSR_OK;
   if (x == nullptr || xs == nullptr || w == nullptr || ws == nullptr || y == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");

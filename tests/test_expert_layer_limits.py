@@ -25,3 +25,14 @@ def test_the_longest_row_fits(chunk, threads):
     chunks = -(-(1 << 25) // chunk)
     assert -(-chunks // 256) <= 65535
     assert (1 << 25) + threads < 1 << 31
+
+
+@pytest.mark.parametrize("k", [(1 << 24) + 16, 1 << 28, 1 << 30])
+def test_sums_longer_than_a_wait_are_refused(k):
+    """A warp waits for a whole tile's sums, two seconds at most: about 0.37 us a slab of 128 values is 3.1 s at k = 2^30."""
+    assert status("bsr_linear_forward_e4m3_block128", A, A, A, A, None, None, A, 8, 8, k, 0, None) == -1
+    assert status("bsr_expert_linear_e4m3_block128", A, A, A, A, None, A, None, A, 8, 8, k, 1, 0, None) == -1
+
+
+def test_the_longest_sum_is_far_inside_a_wait():
+    assert (1 << 24) / 128 * 0.37e-6 < 2.0 / 40

@@ -48,10 +48,10 @@ typedef enum {
   BSR_ERR_UNSUPPORTED = -2,         /* valid request this build does not implement */
   BSR_ERR_WORKSPACE_TOO_SMALL = -3,
   BSR_ERR_CUDA = -4,                /* a CUDA runtime/driver call failed; see bsr_last_error */
-  BSR_ERR_DEVICE_TIMEOUT = -5,      /* a bounded device-side wait gave up (reported by bsr_sync_status) */
+  BSR_ERR_DEVICE_TIMEOUT = -5,      /* a bounded device-side wait gave up (reported by bsr_sync_status, bsr_standalone_status) */
   BSR_ERR_NONFINITE = -6,           /* loss was not finite (reported by bsr_sync_status) */
   BSR_ERR_MEMORY_GUARD = -7,        /* a guard word between two workspace slices was overwritten (bsr_sync_status) */
-  BSR_ERR_DEVICE_CHECK = -8         /* an index check of the checked build (-DBSR_DEBUG) failed (bsr_sync_status) */
+  BSR_ERR_DEVICE_CHECK = -8         /* an index check of the checked build (-DBSR_DEBUG) failed (reported as a wait that gave up) */
 } bsr_status;
 
 enum { BSR_DTYPE_FP32 = 0, BSR_DTYPE_BF16 = 1 };
@@ -243,12 +243,19 @@ int32_t bsr_get_footprint(const bsr_handle* h, bsr_footprint* out_host);
  * finite.  Clears the status word (an overwritten guard stays overwritten and is reported again). */
 int32_t bsr_sync_status(bsr_handle* h, void* stream);
 
+/* The same for the calls that take no handle (stand-alone products, attention, selection, an expert layer's calls).  They return before
+ * their kernels run, so a wait that gives up there leaves outputs incomplete behind a BSR_OK; the kernel raises a bit in one word a
+ * device.  This call synchronises `stream`, reads the current device's word and clears it: BSR_OK, BSR_ERR_DEVICE_TIMEOUT or
+ * BSR_ERR_DEVICE_CHECK, for all such calls that have ended since it was last read, whatever their stream.  Not for a stream
+ * under capture.  The word's address is looked up by the first such call on a device. */
+int32_t bsr_standalone_status(void* stream);
+
 /* Diagnostic of the failure path (no counterpart in the paper).  Every device-side wait of the tensor-core kernels
  * is bounded; when one expires the CTA raises a status bit, frees its tensor memory and returns, and the next
  * bsr_sync_status reports BSR_ERR_DEVICE_TIMEOUT with the context still usable.  This call runs exactly that path on
  * purpose: it enqueues one CTA that waits, for at most limit_ns nanoseconds (1e3 .. 1e8), on a barrier nothing ever
  * arrives at.  Nothing faults and nothing hangs; the following bsr_sync_status returns BSR_ERR_DEVICE_TIMEOUT and
- * clears the status word.  bf16 handles only. */
+ * clears the status word.  bf16 handles only.  With h NULL it raises the word that bsr_standalone_status reads. */
 int32_t bsr_selftest_wait_expiry(bsr_handle* h, uint64_t limit_ns, void* stream);
 
 /* Which kernels run the dense contractions and attention of a bf16 handle (no counterpart in the paper):

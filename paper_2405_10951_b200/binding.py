@@ -27,7 +27,7 @@ STATUS_NAMES = {0: "BSR_OK", -1: "BSR_ERR_INVALID_ARG", -2: "BSR_ERR_UNSUPPORTED
 
 EXPORTS = ["bsr_token_schedule", "bsr_workspace_bytes", "bsr_create", "bsr_destroy", "bsr_last_error", "bsr_set_param",
            "bsr_get_tensor", "bsr_set_lr", "bsr_set_step", "bsr_train_step", "bsr_train_steps", "bsr_train_step_host", "bsr_forward_backward", "bsr_grad_buffer", "bsr_optimizer_step", "bsr_eval_forward", "bsr_get_footprint",
-           "bsr_sync_status", "bsr_selftest_wait_expiry", "bsr_set_gemm_mode", "bsr_set_graph_mode", "bsr_profile_enable", "bsr_profile_read", "bsr_profile_launches", "bsr_token_select", "bsr_gather_fuse", "bsr_linear_forward", "bsr_linear_forward_e4m3", "bsr_linear_backward",
+           "bsr_sync_status", "bsr_standalone_status", "bsr_selftest_wait_expiry", "bsr_set_gemm_mode", "bsr_set_graph_mode", "bsr_profile_enable", "bsr_profile_read", "bsr_profile_launches", "bsr_token_select", "bsr_gather_fuse", "bsr_linear_forward", "bsr_linear_forward_e4m3", "bsr_linear_backward",
            "bsr_linear_backward_static", "bsr_static_last_error", "bsr_attention_forward", "bsr_attention_backward",
            "bsr_e4m3_scale_stride", "bsr_expert_sort", "bsr_expert_scatter", "bsr_expert_scatter_e4m3", "bsr_expert_combine", "bsr_expert_combine_backward",
            "bsr_quantize_e4m3_rows128", "bsr_quantize_e4m3_blocks128", "bsr_linear_forward_e4m3_block128", "bsr_expert_linear_e4m3_block128"]
@@ -103,6 +103,7 @@ def lib() -> C.CDLL:
         L.bsr_eval_forward.argtypes = [vp, vp, i32p, i32, vp, f32p, i32p]
         L.bsr_get_footprint.argtypes = [vp, C.POINTER(bsr_footprint)]
         L.bsr_sync_status.argtypes = [vp, vp]
+        L.bsr_standalone_status.argtypes = [vp]
         L.bsr_selftest_wait_expiry.argtypes = [vp, C.c_uint64, vp]
         L.bsr_set_gemm_mode.argtypes = [vp, i32]
         L.bsr_set_graph_mode.argtypes = [vp, i32]
@@ -293,6 +294,17 @@ def bsr_attention_backward(qkv, dout, lse, score_grad=None, use_tensor_cores: bo
     _check(lib().bsr_attention_backward(_ptr(qkv), _ptr(dout), _ptr(lse), _ptr(score_grad), dt, B, T, H, d, _ptr(dqkv), _ptr(delta),
                                         int(use_tensor_cores), _stream()))
     return dqkv
+
+
+def bsr_standalone_status():
+    """Waits for the current stream and raises BsrError if a kernel of a call without a handle gave up a bounded wait (or failed an index
+    check of the checked build) on the current device since the last time; its outputs are incomplete then."""
+    _check(lib().bsr_standalone_status(_stream()))
+
+
+def bsr_selftest_wait_expiry(limit_ns: int):
+    """Makes a wait without a handle run out; the next bsr_standalone_status reports it."""
+    _check(lib().bsr_selftest_wait_expiry(None, limit_ns, _stream()))
 
 
 # ---- rows of an expert layer, products in 8-bit blocks of 128 -----------------------------------

@@ -4,6 +4,7 @@
 // gradient / AdamW moments of the trainable parameters (flat arrays), the activations the trainable
 // blocks keep for their backward pass, and scratch shared by all blocks.  Frozen blocks write nothing
 // that outlives them (paper Fig. 2: gradient propagation stops at the earliest trainable block).
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -987,6 +988,27 @@ int check_batch(bsr_handle* h, const void* images, int batch) {
 
 }  // namespace
 
+namespace bsr {
+
+// Calls without a handle have no workspace for a status word: they share one a device, in the library's image.  Its address is asked for
+// once a device; null where the runtime does not give it (their kernels then raise nothing).
+static __device__ int g_standalone_status;
+
+int* standalone_status_word(int dev) {
+  static std::atomic<int*> known[64];
+  if (dev < 0 || dev >= 64) return nullptr;
+  int* p = known[dev].load(std::memory_order_acquire);
+  if (p != nullptr) return p;
+  if (cudaGetSymbolAddress((void**)&p, g_standalone_status) != cudaSuccess) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  known[dev].store(p, std::memory_order_release);
+  return p;
+}
+
+}  // namespace bsr
+
 // =================================================================================================
 // C ABI
 // =================================================================================================
@@ -1577,6 +1599,8 @@ int32_t bsr_get_footprint(const bsr_handle* h, bsr_footprint* out) {
   return BSR_OK;
 }
 
+static Ctx bare_ctx(int dtype, void* stream);
+
 int32_t bsr_sync_status(bsr_handle* h, void* stream) {
   if (h == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "handle is null");
   int st = 0;
@@ -1595,11 +1619,10 @@ int32_t bsr_sync_status(bsr_handle* h, void* stream) {
 }
 
 int32_t bsr_selftest_wait_expiry(bsr_handle* h, uint64_t limit_ns, void* stream) {
-  if (h == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "handle is null");
-  if (limit_ns < 1000 || limit_ns > 100000000ull) return set_err(h->err, BSR_ERR_INVALID_ARG, "limit_ns must lie in [1e3, 1e8]");
-  if (h->cfg.dims.dtype != BSR_DTYPE_BF16) return set_err(h->err, BSR_ERR_UNSUPPORTED, "only bf16 handles run kernels with bounded waits");
-  Ctx c = make_ctx(h, stream);
-  wait_expiry_selftest(c, limit_ns);
+  char* err = h != nullptr ? h->err : g_error;
+  if (limit_ns < 1000 || limit_ns > 100000000ull) return set_err(err, BSR_ERR_INVALID_ARG, "limit_ns must lie in [1e3, 1e8]");
+  if (h != nullptr && h->cfg.dims.dtype != BSR_DTYPE_BF16) return set_err(err, BSR_ERR_UNSUPPORTED, "only bf16 handles run kernels with bounded waits");
+  wait_expiry_selftest(h != nullptr ? make_ctx(h, stream) : bare_ctx(BSR_DTYPE_BF16, stream), limit_ns);
   return check_cuda(h, "bsr_selftest_wait_expiry");
 }
 
@@ -1668,8 +1691,28 @@ static Ctx bare_ctx(int dtype, void* stream) {
   c.sm_count = 0;
   c.use_tc = 0;
   int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) c.sm_count = sms;
+  if (cudaGetDevice(&dev) != cudaSuccess) return c;
+  c.status = bsr::standalone_status_word(dev);
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) c.sm_count = sms;
   return c;
+}
+
+int32_t bsr_standalone_status(void* stream) {
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing((cudaStream_t)stream, &capturing) == cudaSuccess && capturing != cudaStreamCaptureStatusNone)
+    return set_err(g_error, BSR_ERR_INVALID_ARG, "bsr_standalone_status: the stream is being captured");
+  int* word = bare_ctx(BSR_DTYPE_FP32, stream).status;
+  int st = 0;
+  cudaError_t e = word != nullptr ? cudaMemcpyAsync(&st, word, 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream) : cudaErrorNoDevice;
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+  if (e == cudaSuccess && st != 0) {         // (what a kernel raises in between is already reported; a word without bits is left alone)
+    e = cudaMemsetAsync(word, 0, 4, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+  }
+  if (e != cudaSuccess) return set_err(g_error, BSR_ERR_CUDA, "bsr_standalone_status: %s", cudaGetErrorString(e));
+  if (st & STATUS_TIMEOUT) return set_err(g_error, BSR_ERR_DEVICE_TIMEOUT, "a bounded device-side wait expired in a call without a handle");
+  if (st & STATUS_CHECK) return set_err(g_error, BSR_ERR_DEVICE_CHECK, "a device-side index check failed (checked build) in a call without a handle");
+  return BSR_OK;
 }
 
 int32_t bsr_token_select(const float* p, int32_t batch, int32_t heads, int32_t m, int32_t k, float* scores, int32_t* kept,

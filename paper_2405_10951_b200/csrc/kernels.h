@@ -50,7 +50,7 @@ struct SideLane {
 struct Ctx {
   cudaStream_t stream;
   int dtype;        // 0 fp32, 1 bf16
-  int* status;      // device status word (may be null for the stand-alone entry points)
+  int* status;      // device status word (may be null)
   int sm_count;
   int use_tc;       // bf16 only: dense contractions on the tcgen05 kernels
   float* split_ws = nullptr;       // scratch for split-k partial sums (optional)
@@ -58,6 +58,9 @@ struct Ctx {
   GemmProfile* prof = nullptr;
   SideLane* side = nullptr;        // optional second lane for optimiser-only reductions
 };
+
+// The status word of calls without a handle on device `dev`, which has to be the current one (null: there is none).
+int* standalone_status_word(int dev);
 
 // The main stream is about to rewrite buffer `which`: wait for the side reduction that may still read it.
 inline void side_join(const Ctx& c, int which) {

@@ -29,7 +29,7 @@ int g_sm_count[MAX_DEVICES] = {0};
 thread_local char g_noalloc_error[256] = "no error";
 
 // Once per device, with that device current: resolve the array's device address.
-int scratch_for_current_device(float** out, int* sms) {
+int scratch_for_current_device(float** out, int* sms, int** status) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) {
     snprintf(g_noalloc_error, sizeof(g_noalloc_error), "no current CUDA device with an ordinal below %d", MAX_DEVICES);
@@ -53,6 +53,7 @@ int scratch_for_current_device(float** out, int* sms) {
   }
   *out = g_scratch_ptr[dev];
   *sms = g_sm_count[dev];
+  *status = bsr::standalone_status_word(dev);
   return 0;
 }
 
@@ -79,12 +80,12 @@ int32_t bsr_linear_backward_static(const void* x, const void* w, const void* dy,
     return BSR_ERR_WORKSPACE_TOO_SMALL;
   }
   float* scratch = nullptr;
-  int sms = 0;
-  if (scratch_for_current_device(&scratch, &sms) != 0) return BSR_ERR_CUDA;   // the message says which step failed
+  int sms = 0, *status = nullptr;
+  if (scratch_for_current_device(&scratch, &sms, &status) != 0) return BSR_ERR_CUDA;   // the message says which step failed
   Ctx c;
   c.stream = (cudaStream_t)stream;
   c.dtype = BSR_DTYPE_BF16;
-  c.status = nullptr;
+  c.status = status;
   c.sm_count = sms;
   c.use_tc = 1;
   GemmEpilogue none;

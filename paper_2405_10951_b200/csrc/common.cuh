@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+#include <mutex>
 #include <utility>
 
 namespace bsr {
@@ -161,17 +163,21 @@ static inline void launch_k(void (*kern)(KArgs...), dim3 grid, dim3 block, size_
 }
 
 // The dynamic shared-memory limit of a kernel is an attribute of the (kernel, device) pair, so the largest value set so
-// far is remembered per device ordinal.  It only grows: launches captured earlier in a graph keep working.
+// far is remembered per device ordinal.  It only grows: launches captured earlier in a graph keep working.  Threads that raise it take
+// turns, or a smaller value could end up in the attribute behind a larger one that is remembered.
 struct SmemLimit {
-  size_t set[64] = {};
+  std::atomic<size_t> set[64] = {};
+  std::mutex raising;
 };
 template <typename Kernel>
 static inline bool ensure_smem(SmemLimit& lim, Kernel kern, size_t bytes) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
-  if (bytes > lim.set[dev]) {
+  if (bytes <= lim.set[dev].load(std::memory_order_acquire)) return true;
+  std::lock_guard<std::mutex> turn(lim.raising);
+  if (bytes > lim.set[dev].load(std::memory_order_relaxed)) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
-    lim.set[dev] = bytes;
+    lim.set[dev].store(bytes, std::memory_order_release);
   }
   return true;
 }

@@ -360,9 +360,18 @@ def _float_type(T, name, t):
 
 
 def _sizes(name, t, dims):
-    if t.dim() != dims:
-        raise BsrError(-1, f"{name} must have {dims} dimensions, not {t.dim()}")
-    return t.shape
+    shape = t.shape
+    if len(shape) != dims:
+        raise BsrError(-1, f"{name} must have {dims} dimensions, not {len(shape)}")
+    if max(shape) >= 1 << 31:
+        raise BsrError(-1, f"{name} has {tuple(shape)} values: sizes must be below 2^31")     # (ctypes would drop the upper bits)
+    return shape
+
+
+def _number(name, v):
+    if not -(1 << 31) <= v < 1 << 31:
+        raise BsrError(-1, f"{name} must be below 2^31, not {v}")
+    return v
 
 
 def bsr_e4m3_scale_stride(k: int) -> int:
@@ -374,7 +383,7 @@ def bsr_expert_sort(expert, experts: int, pos=None, seg_start=None):
     """expert: int32 [tokens, top_k], values outside [0, experts) for slots without an expert.  Returns (pos [tokens, top_k], seg_start
     [experts + 1]) int32."""
     T = _th()
-    shape = _sizes("expert", expert, 2)
+    shape, experts = _sizes("expert", expert, 2), _number("experts", experts)
     pe = _takes("expert", expert, T.i32, shape)
     if pos is None:
         pos = T.empty_like(expert)
@@ -476,7 +485,7 @@ def bsr_quantize_e4m3_blocks128(w, transposed: bool = False, q=None, scale=None,
     T = _th()
     if w.dim() not in (2, 3):
         raise BsrError(-1, "w must be [n, k] or [count, n, k]")
-    n, k = w.shape[-2:]
+    n, k = _sizes("w", w, w.dim())[-2:]
     stack = tuple(w.shape[:-2])
     dt = _float_type(T, "w", w)
     pw = _takes("w", w, w.dtype, stack + (n, k))
@@ -509,7 +518,7 @@ def bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, bias=None, act: int = ACT_N
     _sizes("wq", wq, 2)
     y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (), bias, z, y)
     stream = _run_on(T, xq, xs, wq, ws, bias, z, y)
-    _check((_lib or lib()).bsr_linear_forward_e4m3_block128(*at, *sizes, act, stream))
+    _check((_lib or lib()).bsr_linear_forward_e4m3_block128(*at, *sizes, _number("act", act), stream))
     return y
 
 
@@ -521,7 +530,7 @@ def bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg_start, bias=None, act: i
     y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (experts,), bias, z, y)
     pseg = _takes("seg_start", seg_start, T.i32, (experts + 1,))
     stream = _run_on(T, xq, xs, wq, ws, seg_start, bias, z, y)
-    _check((_lib or lib()).bsr_expert_linear_e4m3_block128(*at[:5], pseg, *at[5:], *sizes, experts, act, stream))
+    _check((_lib or lib()).bsr_expert_linear_e4m3_block128(*at[:5], pseg, *at[5:], *sizes, experts, _number("act", act), stream))
     return y
 
 

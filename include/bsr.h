@@ -457,7 +457,8 @@ int32_t bsr_linear_forward_e4m3_block128(const void* x_codes_dev, const void* x_
                                          void* stream);
 /* The same over rows sorted by expert: the rows seg_start[e] .. seg_start[e + 1] - 1 of x [m, k] with w [experts, n, k][e] and bias
  * [experts, n][e].  Rows of y and z outside every segment stay as they were.  1 <= experts <= 1024, experts * n < 2^31; seg_start
- * as bsr_expert_sort writes it (what lies outside [0, m] is cut, and a row that two segments name is the later one's). */
+ * as bsr_expert_sort writes it (what lies outside [0, m] is cut, and a segment that reaches behind the beginning of a later one ends
+ * there: rows that it alone names behind that one's end stay as they were). */
 int32_t bsr_expert_linear_e4m3_block128(const void* x_codes_dev, const void* x_scale_dev, const void* w_codes_dev, const void* w_scale_dev,
                                         const float* bias_dev, const int32_t* seg_start_dev, void* z_dev, void* y_dev, int32_t m, int32_t n,
                                         int32_t k, int32_t experts, int32_t act, void* stream);

@@ -220,9 +220,10 @@ struct Scales {
 // 32 columns).
 //
 // GELU(z) = max(z, 0) - |z| Phi(-|z|) and GELU'(z) = Phi(z) + z phi(z), with Phi(-t) = exp(-t^2 / 2) R(t).  R falls from 1/2 and goes as
-// 1 / t: it is u (c1 + c2 u + .. + c5 u^4) in u = 1 / (1 + 0.37677 t), fitted to erfcx in double precision by relative error, 2.9e-5 over
-// 0 <= t <= 14, beyond which the exponential is zero: a hundredth of the rounding to bf16, and of every value, where a polynomial
-// for Phi itself is off by a fixed amount.  s = -min(|z|, 16): beyond, the exponential is zero, and so are its products with s, for infinities too.
+// 1 / t: it is c0 + c1 u + .. + c5 u^5 in u = 1 / (1 + 0.36015 t), fitted to erfcx in double precision by relative error, 1.1e-5 over
+// 0 <= t <= 13.3, beyond which the exponential is zero: a 350th of the rounding to bf16, and of every value, where a polynomial
+// for Phi itself is off by a fixed amount.  (Without c0, u times as many terms is one operation more for 4.0e-6: 25216 x 1536 x 384 45.0 -> 46.2 us.)
+// s = -min(|z|, 16): beyond, the exponential is zero, and so are its products with s, for infinities too.
 // Two values at a time, packed wherever an instruction takes pairs (618 -> 541 instructions for 32 rows x 32 columns with the rest: 25216 x 1536 x 384 41.9 -> 37.5 us).
 __device__ __forceinline__ void phi_tail2(uint64_t z, float z0, float z1, uint64_t& s, uint64_t& p, float& e0, float& e1) {
   float h0, h1, d0, d1, u0, u1;
@@ -230,16 +231,17 @@ __device__ __forceinline__ void phi_tail2(uint64_t z, float z0, float z1, uint64
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(h0));
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(h1));
   s = pack2(fmaxf(-fabsf(z0), -16.f), fmaxf(-fabsf(z1), -16.f));
-  unpack2(fma2(s, dup2(-0.37676923076923075f), dup2(1.0f)), d0, d1);
+  unpack2(fma2(s, dup2(-0.3601517975330353f), dup2(1.0f)), d0, d1);
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u0) : "f"(d0));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(u1) : "f"(d1));
   const uint64_t u = pack2(u0, u1);
-  uint64_t r = dup2(-0.09088445f);
-  r = fma2(r, u, dup2(0.19726645f));
-  r = fma2(r, u, dup2(0.0858145f));
-  r = fma2(r, u, dup2(0.15798381f));
-  r = fma2(r, u, dup2(0.14980525f));
-  p = mul2(mul2(r, u), pack2(e0, e1));
+  uint64_t r = dup2(-0.099203065f);
+  r = fma2(r, u, dup2(0.2558196f));
+  r = fma2(r, u, dup2(0.03368386f));
+  r = fma2(r, u, dup2(0.16946077f));
+  r = fma2(r, u, dup2(0.1400296f));
+  r = fma2(r, u, dup2(0.00020378547f));
+  p = mul2(r, pack2(e0, e1));
 }
 __device__ __forceinline__ void gelu2(float& z0, float& z1) {
   uint64_t s, p;

@@ -463,6 +463,10 @@ int32_t bsr_expert_linear_e4m3_block128(const void* x_codes_dev, const void* x_s
                                         const float* bias_dev, const int32_t* seg_start_dev, void* z_dev, void* y_dev, int32_t m, int32_t n,
                                         int32_t k, int32_t experts, int32_t act, void* stream);
 
+/* Diagnostic: how a product of these sizes is cut (experts 0: the dense one).  cut_out [3]: the kernel (0 = a CTA a tile, 1 = a pair of CTAs a tile,
+ * 2 = a tile's k over the CTAs of a cluster), columns a tile, CTAs that share a tile's k.  Launches nothing; without a device, as for 148 SMs. */
+int32_t bsr_e4m3_block128_cut(int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, int32_t* cut_out);
+
 #ifdef __cplusplus
 }
 #endif

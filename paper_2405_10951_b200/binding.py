@@ -30,7 +30,7 @@ EXPORTS = ["bsr_token_schedule", "bsr_workspace_bytes", "bsr_create", "bsr_destr
            "bsr_sync_status", "bsr_standalone_status", "bsr_selftest_wait_expiry", "bsr_set_gemm_mode", "bsr_set_graph_mode", "bsr_profile_enable", "bsr_profile_read", "bsr_profile_launches", "bsr_token_select", "bsr_gather_fuse", "bsr_linear_forward", "bsr_linear_forward_e4m3", "bsr_linear_backward",
            "bsr_linear_backward_static", "bsr_static_last_error", "bsr_attention_forward", "bsr_attention_backward",
            "bsr_e4m3_scale_stride", "bsr_expert_sort", "bsr_expert_scatter", "bsr_expert_scatter_e4m3", "bsr_expert_combine", "bsr_expert_combine_backward",
-           "bsr_quantize_e4m3_rows128", "bsr_quantize_e4m3_blocks128", "bsr_linear_forward_e4m3_block128", "bsr_expert_linear_e4m3_block128"]
+           "bsr_quantize_e4m3_rows128", "bsr_quantize_e4m3_blocks128", "bsr_linear_forward_e4m3_block128", "bsr_expert_linear_e4m3_block128", "bsr_e4m3_block128_cut"]
 
 
 class bsr_dims(C.Structure):
@@ -129,6 +129,7 @@ def lib() -> C.CDLL:
         L.bsr_quantize_e4m3_blocks128.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
         L.bsr_linear_forward_e4m3_block128.argtypes = [vp, vp, vp, vp, f32p, vp, vp, i32, i32, i32, i32, vp]
         L.bsr_expert_linear_e4m3_block128.argtypes = [vp, vp, vp, vp, f32p, i32p, vp, vp, i32, i32, i32, i32, i32, vp]
+        L.bsr_e4m3_block128_cut.argtypes = [i32, i32, i32, i32, i32, i32p]
         for name in EXPORTS:
             if name not in ("bsr_last_error", "bsr_static_last_error"):
                 getattr(L, name).restype = C.c_int32
@@ -532,6 +533,13 @@ def bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg_start, bias=None, act: i
     stream = _run_on(T, xq, xs, wq, ws, seg_start, bias, z, y)
     _check((_lib or lib()).bsr_expert_linear_e4m3_block128(*at[:5], pseg, *at[5:], *sizes, experts, _number("act", act), stream))
     return y
+
+
+def bsr_e4m3_block128_cut(m: int, n: int, k: int, experts: int = 0, act: int = ACT_NONE):
+    """(kernel, columns a tile, CTAs that share a tile's k) of a product of these sizes; kernel 0: a CTA a tile, 1: a pair of CTAs, 2: k over a cluster."""
+    cut = (C.c_int32 * 3)()
+    _check(lib().bsr_e4m3_block128_cut(*(_number("a size", v) for v in (m, n, k, experts, act)), cut))
+    return tuple(cut)
 
 
 class Engine:

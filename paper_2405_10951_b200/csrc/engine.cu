@@ -1931,14 +1931,22 @@ int32_t bsr_quantize_e4m3_blocks128(const void* w, int32_t dtype, int32_t count,
   return check_cuda(nullptr, "bsr_quantize_e4m3_blocks128");
 }
 
-static int32_t linear_block128(const char* what, const void* x, const void* xs, const void* w, const void* ws, const float* bias, const int32_t* seg_start, void* z, void* y,
-                               int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, void* stream) {
+static int check_product(int32_t m, int32_t n, int32_t k, int32_t act) {
   // Sizes that a round up to a tile keeps within 31 bits; sums that end long before a wait for them does (a slab of 128 values takes a CTA
   // about 0.37 us, so 2^24 values 48 ms of the two seconds that a wait may last; and their accumulator drops a 16th of them at most).
   constexpr int32_t LARGEST = 1 << 30, LONGEST_SUM = 1 << 24;
   if (m < 0 || n < 8 || n % 8 != 0 || k < 16 || k % 16 != 0 || m > LARGEST || n > LARGEST || k > LONGEST_SUM)
     return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 0, n a multiple of 8, each at most 2^30, and k a multiple of 16 up to 2^24");
   if (act < BSR_ACT_NONE || act > BSR_ACT_GELU_GRAD) return set_err(g_error, BSR_ERR_INVALID_ARG, "bad act");
+  return BSR_OK;
+}
+static int check_experts(int32_t n, int32_t experts) {
+  return experts < 1 || experts > 1024 || (int64_t)experts * n > INT32_MAX ? set_err(g_error, BSR_ERR_INVALID_ARG, "need 1 <= experts <= 1024 and experts * n < 2^31") : BSR_OK;
+}
+
+static int32_t linear_block128(const char* what, const void* x, const void* xs, const void* w, const void* ws, const float* bias, const int32_t* seg_start, void* z, void* y,
+                               int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, void* stream) {
+  if (int rc = check_product(m, n, k, act)) return rc;
   if (m == 0) return BSR_OK;
   if (x == nullptr || xs == nullptr || w == nullptr || ws == nullptr || y == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   if (act == BSR_ACT_NONE && z != nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "a pre-activation belongs to an activation");
@@ -1961,9 +1969,19 @@ int32_t bsr_linear_forward_e4m3_block128(const void* x, const void* xs, const vo
 
 int32_t bsr_expert_linear_e4m3_block128(const void* x, const void* xs, const void* w, const void* ws, const float* bias, const int32_t* seg_start, void* z, void* y,
                                         int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, void* stream) {
-  if (experts < 1 || experts > 1024 || (int64_t)experts * n > INT32_MAX) return set_err(g_error, BSR_ERR_INVALID_ARG, "need 1 <= experts <= 1024 and experts * n < 2^31");
+  if (int rc = check_experts(n, experts)) return rc;
   if (seg_start == nullptr && m > 0) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
   return linear_block128("bsr_expert_linear_e4m3_block128", x, xs, w, ws, bias, seg_start, z, y, m, n, k, experts, act, stream);
+}
+
+int32_t bsr_e4m3_block128_cut(int32_t m, int32_t n, int32_t k, int32_t experts, int32_t act, int32_t* cut) {
+  if (cut == nullptr) return set_err(g_error, BSR_ERR_INVALID_ARG, "null argument");
+  if (int rc = check_product(m, n, k, act)) return rc;
+  if (m < 1) return set_err(g_error, BSR_ERR_INVALID_ARG, "need m >= 1");
+  if (experts != 0)
+    if (int rc = check_experts(n, experts)) return rc;
+  block128_cut(bare_ctx(BSR_DTYPE_BF16, nullptr), m, n, k, experts != 0, experts != 0 ? experts : 1, act, cut);
+  return BSR_OK;
 }
 
 }  // extern "C"

@@ -1124,24 +1124,35 @@ static bool make_out_map(CUtensorMap* map, const void* ptr, int n, int m, int co
 //   8192 x 4096 x 7168     193 / 177       8192 x 1024 x 1024    13.5 / 15.8      64 experts of 768 rows, 1408 x 2048: 150 / 133
 //   16 experts, 25216 x 1536 x 768 with GELU: 49.5 / 54.2
 // Experts are taken to have equal shares of the rows (their counts are on the device).
-struct Cut { bool pair; int bn; };
-static Cut choose_cut(int m, int n, int k, int experts, int act, int sms) {
+struct Cut { bool pair; int bn; int splits; };       // splits: of a few-tile product's k; 0: one of the persistent kernels
+static Cut choose_wide_cut(int m, int n, int k, int experts, int act, int sms) {
   const int share = ceil_div(m, experts), kb = ceil_div(k, BK);
   auto tiles = [&](int rows, int cols) { return (long)(experts < m ? experts : m) * ceil_div(share, rows) * ceil_div(n, cols); };
-  if (n <= 64 || tiles(BM, 64) <= sms) return {false, 64};
-  if (n <= 128 || tiles(BM, 128) <= sms) return {false, 128};
+  if (n <= 64 || tiles(BM, 64) <= sms) return {false, 64, 0};
+  if (n <= 128 || tiles(BM, 128) <= sms) return {false, 128, 0};
   auto longer = [](double x, double y) { return x > y ? x : y; };
   const double epi1[3] = {0.0, 3.3, 4.3}, epi2[3] = {0.0, 4.6, 5.3};
-  Cut best = {false, 192};
+  Cut best = {false, 192, 0};
   double t_best = ceil_div(tiles(BM, 192), sms) * longer(0.93 + 0.367 * kb, epi1[act]);
   for (int w = P_WIDTH; w >= 128; w -= 16) {
     const double t = ceil_div(tiles(2 * BM, w), sms / 2) * longer(1.5 + 0.38 * kb * (152 + w / 2) / 272, epi2[act]);
-    if (t < t_best) { t_best = t; best = {true, w}; }
+    if (t < t_best) { t_best = t; best = {true, w, 0}; }
   }
   return best;
 }
+static Cut choose_cut(int m, int n, int k, bool grouped, int experts, int act, int sms) {
+  const int splits = grouped ? 0 : small_splits(m, n, k, sms);
+  return splits > 0 ? Cut{false, S_BN, splits} : choose_wide_cut(m, n, k, experts, act, sms);
+}
 
 }  // namespace tcb
+
+void block128_cut(const Ctx& c, int m, int n, int k, bool grouped, int experts, int act, int* out) {
+  const tcb::Cut cut = tcb::choose_cut(m, n, k, grouped, experts, act, c.sm_count > 0 ? c.sm_count : B200_SMS);
+  out[0] = cut.splits > 0 ? 2 : cut.pair ? 1 : 0;
+  out[1] = cut.bn;
+  out[2] = cut.splits > 0 ? cut.splits : 1;
+}
 
 // y [m, n] bf16 = epilogue(A W^T); see kernels.h.
 int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void* Wq, const void* w_scale, const int* seg_start, int experts, void* C, int m, int n, int k,
@@ -1149,10 +1160,9 @@ int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void*
   using namespace tcb;
   const int sms = c.sm_count > 0 ? c.sm_count : B200_SMS;
   const long some = seg_start != nullptr ? (experts < m ? experts : m) - 1 : 0;      // at most so many tiles more than the rows alone would take
-  const int splits = seg_start == nullptr ? small_splits(m, n, k, sms) : 0;
-  const Cut cut = splits > 0 ? Cut{false, S_BN} : choose_cut(m, n, k, experts, e.act, sms);
+  const Cut cut = choose_cut(m, n, k, seg_start != nullptr, experts, e.act, sms);
   const bool pair = cut.pair;
-  const int bn = cut.bn;
+  const int bn = cut.bn, splits = cut.splits;
   bf16* z = (bf16*)(e.act == 1 ? e.aux_out : const_cast<void*>(e.aux_in));
   CUtensorMap ma, ma32, mw, my, mz;
   if (!make_out_map(&my, C, n, m, chunk_of(e.act)) || !make_out_map(&mz, z != nullptr ? z : C, n, m, chunk_of(e.act))) return -2;

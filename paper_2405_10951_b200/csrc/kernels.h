@@ -329,6 +329,8 @@ void quantize_blocks128(const Ctx& c, const void* w, int count, int n, int k, vo
 // C [m, n] bf16 from codes and scales; seg_start null: dense, experts 1.  e: bias ([experts][n]), act, aux_out, aux_in.
 int gemm_block128(const Ctx& c, const void* Aq, const void* a_scale, const void* Wq, const void* w_scale, const int* seg_start, int experts, void* C, int m, int n, int k,
                   const GemmEpilogue& e);
+// How it cuts such a product: the kernel (0: a CTA a tile, 1: two, 2: k over a cluster), columns a tile, CTAs that share a tile's k.
+void block128_cut(const Ctx& c, int m, int n, int k, bool grouped, int experts, int act, int* out);
 
 // ---- guard words between workspace slices ------------------------------------------------------
 // table[i]: byte offset from base of guard i (words 32-bit values each).  guards_write fills them with `word`;

@@ -121,7 +121,7 @@ quantize_blocks128_kernel(const T* __restrict__ w, int n, int k, uint8_t* __rest
     }
   }
   // scales: the thread of the block's first column writes its byte, the last block's threads the padding behind it
-  const int kblocks = (k + 127) / 128, nblocks = (n + 127) / 128;
+  const int kblocks = (k - 1) / 128 + 1, nblocks = (n - 1) / 128 + 1;       // (k may lie within 127 of 2^31)
   if (threadIdx.x == 0) scale[(mat * nblocks + nb) * stride + kb] = (uint8_t)byte;
   if (kb == kblocks - 1 && threadIdx.x < stride - kblocks) scale[(mat * nblocks + nb) * stride + kblocks + threadIdx.x] = 127;
   if (qt == nullptr) return;

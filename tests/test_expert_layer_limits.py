@@ -36,3 +36,20 @@ def test_sums_longer_than_a_wait_are_refused(k):
 
 def test_the_longest_sum_is_far_inside_a_wait():
     assert (1 << 24) / 128 * 0.37e-6 < 2.0 / 40
+
+
+@pytest.mark.gpu
+def test_quantised_rows_up_to_the_last_block_of_31_bits():
+    """k within 127 of 2^31: the number of blocks along k does not pass 31 bits on the way."""
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    k = (1 << 31) - 16
+    w = torch.zeros((1, k), dtype=torch.bfloat16, device="cuda")
+    w[0, k - 1], w[0, k - 112], w[0, k - 113], w[0, 5] = 448.0, 3.0, -896.0, 1.0
+    for q, scale in (Bd.bsr_quantize_e4m3_blocks128(w), Bd.bsr_quantize_e4m3_rows128(w)):
+        assert scale.shape == (1, 1 << 24)
+        at = [0, 1, (1 << 24) - 3, (1 << 24) - 2, (1 << 24) - 1]
+        assert scale[0, at].tolist() == [119, 127, 127, 128, 127]
+        code = q.view(torch.uint8)[0, [5, k - 113, k - 112, k - 1]]
+        assert code.view(torch.float8_e4m3fn).float().tolist() == [256.0, -448.0, 3.0, 448.0]
+        del q, scale

@@ -361,18 +361,14 @@ def _float_type(T, name, t):
 
 
 def _sizes(name, t, dims):
-    shape = t.shape
-    if len(shape) != dims:
-        raise BsrError(-1, f"{name} must have {dims} dimensions, not {len(shape)}")
-    if max(shape) >= 1 << 31:
-        raise BsrError(-1, f"{name} has {tuple(shape)} values: sizes must be below 2^31")     # (ctypes would drop the upper bits)
-    return shape
+    if t.dim() != dims:
+        raise BsrError(-1, f"{name} must have {dims} dimensions, not {t.dim()}")
+    return t.shape
 
 
-def _number(name, v):
-    if not -(1 << 31) <= v < 1 << 31:
-        raise BsrError(-1, f"{name} must be below 2^31, not {v}")
-    return v
+def _too_large(*numbers):
+    """For a call whose numbers, or'ed together, do not fit 31 bits: ctypes would drop the upper ones."""
+    raise BsrError(-1, f"sizes must be below 2^31 and not negative, not {numbers}")
 
 
 def bsr_e4m3_scale_stride(k: int) -> int:
@@ -384,7 +380,9 @@ def bsr_expert_sort(expert, experts: int, pos=None, seg_start=None):
     """expert: int32 [tokens, top_k], values outside [0, experts) for slots without an expert.  Returns (pos [tokens, top_k], seg_start
     [experts + 1]) int32."""
     T = _th()
-    shape, experts = _sizes("expert", expert, 2), _number("experts", experts)
+    tokens, top_k = shape = _sizes("expert", expert, 2)
+    if (tokens | top_k | experts) >> 31:
+        _too_large(tokens, top_k, experts)
     pe = _takes("expert", expert, T.i32, shape)
     if pos is None:
         pos = T.empty_like(expert)
@@ -392,7 +390,7 @@ def bsr_expert_sort(expert, experts: int, pos=None, seg_start=None):
         seg_start = T.empty(max(experts, 0) + 1, dtype=T.i32, device=expert.device)
     pp, ps = _takes("pos", pos, T.i32, shape), _takes("seg_start", seg_start, T.i32, (experts + 1,))
     stream = _run_on(T, expert, pos, seg_start)
-    _check((_lib or lib()).bsr_expert_sort(pe, shape[0], shape[1], experts, pp, ps, stream))
+    _check((_lib or lib()).bsr_expert_sort(pe, tokens, top_k, experts, pp, ps, stream))
     return pos, seg_start
 
 
@@ -401,6 +399,8 @@ def bsr_expert_scatter(x, pos, rows=None):
     T = _th()
     tokens, dim = _sizes("x", x, 2)
     top_k = _sizes("pos", pos, 2)[1]
+    if (tokens | dim | top_k) >> 31:
+        _too_large(tokens, dim, top_k)
     dt = _float_type(T, "x", x)
     if rows is None:
         rows = T.empty((tokens * top_k, dim), dtype=x.dtype, device=x.device)
@@ -415,6 +415,8 @@ def bsr_expert_scatter_e4m3(x, pos, q=None, scale=None):
     T = _th()
     tokens, dim = _sizes("x", x, 2)
     top_k = _sizes("pos", pos, 2)[1]
+    if (tokens | dim | top_k) >> 31:
+        _too_large(tokens, dim, top_k)
     dt = _float_type(T, "x", x)
     px, pp = _takes("x", x, x.dtype, (tokens, dim)), _takes("pos", pos, T.i32, (tokens, top_k))
     q, scale, pq, ps = _codes_out(T, x, (), tokens * top_k, dim, tokens * top_k, q, scale)
@@ -429,6 +431,8 @@ def bsr_expert_combine(rows, pos, weights=None, residual=None, out=None, dtype=N
     T = _th()
     tokens, top_k = _sizes("pos", pos, 2)
     dim = _sizes("rows", rows, 2)[1]
+    if (tokens | dim | top_k) >> 31:
+        _too_large(tokens, dim, top_k)
     if out is None:
         out = T.empty((tokens, dim), dtype=residual.dtype if residual is not None else dtype or rows.dtype, device=rows.device)
     rt, ot = _float_type(T, "rows", rows), _float_type(T, "out", out)
@@ -445,6 +449,8 @@ def bsr_expert_combine_backward(dout, rows, pos, weights, drows=None, dw=None):
     T = _th()
     tokens, top_k = _sizes("pos", pos, 2)
     dim = _sizes("rows", rows, 2)[1]
+    if (tokens | dim | top_k) >> 31:
+        _too_large(tokens, dim, top_k)
     if drows is None:
         drows = T.empty_like(rows)
     if dw is None:
@@ -472,6 +478,8 @@ def bsr_quantize_e4m3_rows128(x, q=None, scale=None):
     """x [m, k] to (codes [m, k] float8_e4m3fn, scales [m, stride] uint8)."""
     T = _th()
     m, k = _sizes("x", x, 2)
+    if (m | k) >> 31:
+        _too_large(m, k)
     dt = _float_type(T, "x", x)
     px = _takes("x", x, x.dtype, (m, k))
     q, scale, pq, ps = _codes_out(T, x, (), m, k, m, q, scale)
@@ -486,8 +494,11 @@ def bsr_quantize_e4m3_blocks128(w, transposed: bool = False, q=None, scale=None,
     T = _th()
     if w.dim() not in (2, 3):
         raise BsrError(-1, "w must be [n, k] or [count, n, k]")
-    n, k = _sizes("w", w, w.dim())[-2:]
+    n, k = w.shape[-2:]
     stack = tuple(w.shape[:-2])
+    count = stack[0] if stack else 1
+    if (count | n | k) >> 31:
+        _too_large(count, n, k)
     dt = _float_type(T, "w", w)
     pw = _takes("w", w, w.dtype, stack + (n, k))
     q, scale, pq, ps = _codes_out(T, w, stack, n, k, (n + 127) // 128, q, scale)
@@ -495,14 +506,16 @@ def bsr_quantize_e4m3_blocks128(w, transposed: bool = False, q=None, scale=None,
     if transposed or qt is not None or scale_t is not None:
         qt, scale_t, pqt, pst = _codes_out(T, w, stack, k, n, (k + 127) // 128, qt, scale_t, "_t")
     stream = _run_on(T, w, q, scale, qt, scale_t)
-    _check((_lib or lib()).bsr_quantize_e4m3_blocks128(pw, dt, stack[0] if stack else 1, n, k, pq, ps, pqt, pst, stream))
+    _check((_lib or lib()).bsr_quantize_e4m3_blocks128(pw, dt, count, n, k, pq, ps, pqt, pst, stream))
     return (q, scale) if qt is None else (q, scale, qt, scale_t)
 
 
-def _block128_operands(T, xq, xs, wq, ws, stack, bias, z, y):
+def _block128_operands(T, xq, xs, wq, ws, stack, bias, z, y, act):
     """y, the sizes and the addresses in the order of the library's arguments (bias, z and y last)."""
     m, k = _sizes("xq", xq, 2)
     n = wq.shape[-2]
+    if (m | n | k | act) >> 31:
+        _too_large(m, n, k, act)
     stride = (k + 511) // 512 * 4
     if y is None:
         y = T.empty((m, n), dtype=T.bf16, device=xq.device)
@@ -517,9 +530,9 @@ def bsr_linear_forward_e4m3_block128(xq, xs, wq, ws, bias=None, act: int = ACT_N
     [m, n] bf16 if that is given; ACT_GELU_GRAD: the product is multiplied by GELU'(z)."""
     T = _th()
     _sizes("wq", wq, 2)
-    y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (), bias, z, y)
+    y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (), bias, z, y, act)
     stream = _run_on(T, xq, xs, wq, ws, bias, z, y)
-    _check((_lib or lib()).bsr_linear_forward_e4m3_block128(*at, *sizes, _number("act", act), stream))
+    _check((_lib or lib()).bsr_linear_forward_e4m3_block128(*at, *sizes, act, stream))
     return y
 
 
@@ -528,17 +541,19 @@ def bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg_start, bias=None, act: i
     z outside every segment stay as they are (a y that is not passed in holds anything there)."""
     T = _th()
     experts = _sizes("wq", wq, 3)[0]
-    y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (experts,), bias, z, y)
+    y, sizes, at = _block128_operands(T, xq, xs, wq, ws, (experts,), bias, z, y, act)
     pseg = _takes("seg_start", seg_start, T.i32, (experts + 1,))
     stream = _run_on(T, xq, xs, wq, ws, seg_start, bias, z, y)
-    _check((_lib or lib()).bsr_expert_linear_e4m3_block128(*at[:5], pseg, *at[5:], *sizes, experts, _number("act", act), stream))
+    _check((_lib or lib()).bsr_expert_linear_e4m3_block128(*at[:5], pseg, *at[5:], *sizes, experts, act, stream))
     return y
 
 
 def bsr_e4m3_block128_cut(m: int, n: int, k: int, experts: int = 0, act: int = ACT_NONE):
     """(kernel, columns a tile, CTAs that share a tile's k) of a product of these sizes; kernel 0: a CTA a tile, 1: a pair of CTAs, 2: k over a cluster."""
+    if (m | n | k | experts | act) >> 31:
+        _too_large(m, n, k, experts, act)
     cut = (C.c_int32 * 3)()
-    _check(lib().bsr_e4m3_block128_cut(*(_number("a size", v) for v in (m, n, k, experts, act)), cut))
+    _check(lib().bsr_e4m3_block128_cut(m, n, k, experts, act, cut))
     return tuple(cut)
 
 

@@ -17,8 +17,9 @@
 //                               for the scales; two of 256 would not)
 //   gemm_block128_pair_kernel   persistent, two CTAs (cta_group::2) a tile of 256 rows and up to 240 columns: long k, many rows
 //   gemm_block128_small_kernel  a tile's k over the CTAs of a cluster: few tiles
-// What bounds them: the tensor pipe where k is long (8192 x 4096 x 7168: busy 84 % of 179 us, 2.68 PFLOP/s; under the power limit 207 us); at k = 768 and below what
-// operand loads, output stores and the tensor core's reads share inside an SM (25216 x 2304 x 768 51.5 us, without stores 45, without an epilogue 39).
+// What bounds them: the tensor pipe where k is long (8192 x 4096 x 7168: 177 us, 2.72 PFLOP/s; under the power limit 216 us); at k = 768 and below what operand
+// loads, output stores and the tensor core's reads share inside an SM (25216 x 2304 x 768 on single CTAs 53.7 us, without stores 38.2, without an
+// epilogue 36.9; on pairs 51.5, 42.7 and 39.9).  A warp waits for a whole tile's sums: k is limited so that they are there long before it gives up.
 // The persistent kernels' warps:
 //   warp 0      : TMA producer (one lane)
 //   warp 1      : tensor-memory allocation, copies of scales to tensor memory, MMA issue (one lane)
@@ -1118,11 +1119,13 @@ static bool make_out_map(CUtensorMap* map, const void* ptr, int n, int m, int co
 // How a product that is not of few tiles is cut: what fits the SMs in one wave takes the narrowest tiles that do; else one CTA or two a tile,
 // and the pair's width, by waves times the time of one.  A wave takes 0.93 us and 0.367 a slab on single CTAs, 1.5 and 0.38 on pairs of 240 columns
 // (narrower ones less: a slab of 160, 192, 240 columns 341, 370, 402 ns where nothing else waits), or, longer, its epilogue (by activation).
-//   us of a launch, one CTA a tile and two:
-//   25216 x 2304 x 384    32.6 / 35.6      25216 x 2304 x 768    50.3 / 51.2      25216 x 2304 x 1536   85.5 / 80.0      6304 x 2304 x 768    16.0 / 17.7
-//   25216 x 768 x 1536    29.5 / 34.9      2048 x 2048 x 4096    22.8 / 17.8      3000 x 1000 x 7168    20.3 / 24.4      4096 x 4096 x 4096   57.0 / 52.7
-//   8192 x 4096 x 7168     193 / 177       8192 x 1024 x 1024    13.5 / 15.8      64 experts of 768 rows, 1408 x 2048: 150 / 133
-//   16 experts, 25216 x 1536 x 768 with GELU: 49.5 / 54.2
+//   us of a launch (thirty in a row on cool clocks), one CTA a tile and two:
+//   25216 x 2304 x 384    35.2 / 35.4      25216 x 2304 x 768    53.7 / 51.5      25216 x 2304 x 1536   85.4 / 80.4      6304 x 2304 x 768    16.7 / 17.8
+//   25216 x 768 x 1536    31.2 / 34.9      2048 x 2048 x 4096    23.6 / 18.6      3000 x 1000 x 7168    22.1 / 25.1      4096 x 4096 x 4096   57.7 / 53.1
+//   8192 x 4096 x 7168     196 / 177       8192 x 1024 x 1024    13.9 / 16.2      64 experts of 768 rows, 1408 x 2048: 152 / 135
+//   16 experts, 25216 x 1536 x 768 with GELU: 50.3 / 55.9
+// Of these the estimate takes the slower side three times: 25216 x 2304 x 768 on single CTAs, 6304 x 2304 x 768 on pairs of 224 and 3000 x 1000 x 7168 on
+// pairs of 176 (it has one slope for all widths and no cost for a short last wave).
 // Experts are taken to have equal shares of the rows (their counts are on the device).
 struct Cut { bool pair; int bn; int splits; };       // splits: of a few-tile product's k; 0: one of the persistent kernels
 static Cut choose_wide_cut(int m, int n, int k, int experts, int act, int sms) {

@@ -13,7 +13,7 @@ namespace bsr {
 
 typedef __nv_bfloat16 bf16;
 
-// Device status word bits (read and cleared by bsr_sync_status).
+// Device status word bits (read and cleared by bsr_sync_status and bsr_standalone_status).
 enum : int { STATUS_TIMEOUT = 1, STATUS_NONFINITE = 2, STATUS_GUARD = 4, STATUS_CHECK = 8 };
 
 // Index checks of the checked build (-DBSR_DEBUG): a failed check raises STATUS_CHECK in the status word (never a trap:

@@ -53,3 +53,25 @@ def test_quantised_rows_up_to_the_last_block_of_31_bits():
         code = q.view(torch.uint8)[0, [5, k - 113, k - 112, k - 1]]
         assert code.view(torch.float8_e4m3fn).float().tolist() == [256.0, -448.0, 3.0, 448.0]
         del q, scale
+
+
+@pytest.mark.gpu
+def test_the_longest_sum_is_there():
+    import torch
+    from paper_2405_10951_b200 import binding as Bd
+    m, n, k = 9, 16, 1 << 24
+    x = torch.zeros((m, k), dtype=torch.bfloat16, device="cuda")
+    for row in range(m):
+        x[row, row * 1000 + 7] = 2.0
+        x[row, k - 1 - row * 130] = -(row + 4.0)
+    w = torch.ones((1, n, k), dtype=torch.bfloat16, device="cuda")
+    w[0, 3, k // 2:] = 0.5
+    xq, xs = Bd.bsr_quantize_e4m3_rows128(x)
+    wq, ws = Bd.bsr_quantize_e4m3_blocks128(w)
+    want = torch.tensor([[2.0 - (row + 4.0) * (0.5 if col == 3 else 1.0) for col in range(n)] for row in range(m)], device="cuda")     # exact in bf16
+    Bd.bsr_standalone_status()
+    seg = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+    assert Bd.bsr_e4m3_block128_cut(m, n, k)[2] == 8 and Bd.bsr_e4m3_block128_cut(m, n, k, 1)[2] == 1      # k over a cluster, and not
+    for y in (Bd.bsr_linear_forward_e4m3_block128(xq, xs, wq[0], ws[0]), Bd.bsr_expert_linear_e4m3_block128(xq, xs, wq, ws, seg)):
+        assert torch.equal(y.float(), want)
+    Bd.bsr_standalone_status()
